@@ -61,7 +61,8 @@ typedef enum {
     PBS_ERR_HIP = 5          /* a kernel launch failed */
 } pbs_status;
 
-typedef enum { PBS_F32 = 0, PBS_BF16 = 1 } pbs_dtype;
+/* PBS_E4M3 (8-bit floating point, 4 exponent and 3 mantissa bits, no infinities) and PBS_I8 are types of a pbs_cache only. */
+typedef enum { PBS_F32 = 0, PBS_BF16 = 1, PBS_E4M3 = 2, PBS_I8 = 3 } pbs_dtype;
 
 /*
  * PBS_FLAG_FORCE_FIRST_BLOCK: Algorithm 2 also keeps key block 0 in every row.
@@ -302,6 +303,131 @@ pbs_status pbs_mass_covered(const pbs_problem *p, const float *lse_listed, const
 pbs_status pbs_mfma_rate_probe(int random_operands, int iters, float *sink, size_t sink_floats, double *flop,
                                void *stream);
 pbs_status pbs_shader_clock_meter(float *out, int micros, void *stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------------------------
+ * Around the prefill path: rotary positions in front of it, the paged key/value cache behind it, and attention of new
+ * tokens over that cache.
+ *
+ * These calls see tensors as tokens x heads x features: element (t, h, e) of a tensor lies at t * strides.token +
+ * h * strides.head + e, in elements; features are consecutive.  [tokens, heads, d] memory has strides {heads * d, d}, the
+ * [1, heads, n, d] memory of the calls above {d, n * d}, and a slice of a fused projection its own.  Base addresses are
+ * 16-byte aligned, strides are not negative and whole multiples of 16 bytes; rows of an output do not overlap (all
+ * PBS_ERR_SHAPE otherwise).  d is 64 or 128.  A count of zero tokens or sequences is a call that does nothing.
+ * The other conventions above hold: host-validated, nothing allocated, no synchronisation, deterministic.
+ */
+typedef struct { int64_t token, head; } pbs_strides;
+
+/*
+ * Rotary positions.  Every head's first `rot` features are taken as rot / 2 pairs, pair e turned by the angle
+ * position * freq[e] and multiplied by `magnitude`; the features behind them are copied:
+ *     first'  = magnitude * (first * cos - second * sin),      second' = magnitude * (first * sin + second * cos).
+ *   layout   PBS_ROPE_HALF: pair e is features (e, e + rot / 2); PBS_ROPE_INTERLEAVED: features (2e, 2e + 1).
+ *   rot      a multiple of 16, at most d.
+ *   flags    PBS_ROPE_TRANSPOSE: sin changes its sign: the gradient of the turned features with respect to the given
+ *            ones, applied to Q and K (with magnitude 1 also the inverse).
+ *   freq     [rot / 2] float64, device memory: radians per position, as pbs_rope_frequencies forms them.
+ *   positions [tokens] int32, device memory, any sign; the same for all heads.
+ *   Q, K     [tokens, h_q, d], [tokens, h_kv, d] of dtype PBS_BF16 or PBS_F32; h_q or h_kv (not both) may be 0, its
+ *            pointers are then ignored.  Qout and Kout may be Q and K themselves with the same strides; other overlaps are
+ *            not allowed.
+ * The angle is formed and reduced to one turn in 64 bits; cos, sin and the products are fp32, rounded once at the end.
+ * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, rot, layout, more than 2^31 - 1 rows), PBS_ERR_HIP.
+ */
+enum { PBS_ROPE_HALF = 0, PBS_ROPE_INTERLEAVED = 1 };
+enum { PBS_ROPE_TRANSPOSE = 1u };
+typedef struct {
+    int32_t tokens, h_q, h_kv, d, rot;
+    int32_t layout;   /* PBS_ROPE_HALF or PBS_ROPE_INTERLEAVED */
+    int32_t dtype;    /* of Q, K, Qout, Kout */
+    float magnitude;  /* 0 means 1 */
+    uint32_t flags;   /* PBS_ROPE_TRANSPOSE */
+    pbs_strides q, k, q_out, k_out;
+} pbs_rope_problem;
+pbs_status pbs_rope(const pbs_rope_problem *p, const double *freq, const int32_t *positions, const void *Q,
+                    const void *K, void *Qout, void *Kout, void *stream);
+
+/*
+ * The frequencies of the rotary pairs, f_e = base^(-2e / rot), and how they are scaled for contexts longer than the
+ * `original` one.  Runs on the host; freq [rot / 2] and magnitude are HOST memory.
+ *   PBS_ROPE_PLAIN   f_e.
+ *   PBS_ROPE_LINEAR  f_e / factor (position interpolation).
+ *   PBS_ROPE_BANDS   by the turns w_e = original * f_e / (2 pi) that a pair makes over the original context: keep =
+ *                    clamp((w_e - low) / (high - low), 0, 1), f_e * (keep + (1 - keep) / factor).
+ *   PBS_ROPE_RAMP    by the pair's index: i(w) = rot * ln(original / (2 pi w)) / (2 ln base), squeeze = clamp((e - a) /
+ *                    max(b - a, 0.001), 0, 1) with a = max(floor(i(high)), 0), b = min(ceil(i(low)), rot - 1),
+ *                    f_e * (1 - squeeze + squeeze / factor), and magnitude 0.1 ln(factor) + 1 (arXiv 2309.00071).
+ * *magnitude receives 1 for the other three.  Errors: PBS_ERR_NULL; PBS_ERR_SHAPE unless rot is even and positive, base > 1,
+ * factor >= 1, original >= 1 and 0 < low < high (each looked at where it is used); PBS_ERR_UNSUPPORTED for an unknown scaling.
+ */
+enum { PBS_ROPE_PLAIN = 0, PBS_ROPE_LINEAR = 1, PBS_ROPE_BANDS = 2, PBS_ROPE_RAMP = 3 };
+pbs_status pbs_rope_frequencies(int scaling, int32_t rot, double base, double factor, double original, double low,
+                                double high, double *freq, double *magnitude);
+
+/*
+ * A paged key/value cache.  Slot s = page number * page + place in the page holds one token's keys and values of every kv
+ * head: row (h, place) of page K[page number], of `d` features.  What a row holds, for K and V alike:
+ *   PBS_BF16   the features themselves; k_scale and v_scale are NULL.
+ *   PBS_E4M3, PBS_I8   a factor f = max(|largest feature| / M, 2^-126) in fp32, M = 448 and 127, and every feature divided by f
+ *              and rounded to the nearest value of the type, ties to even; the row stands for the products with f.  A
+ *              row with an infinite or NaN feature holds the factor NaN and zeros: it reads back as NaN throughout.
+ * K, V: device memory, 16-byte aligned, caller-owned like everything else.
+ */
+typedef struct {
+    int32_t pages;     /* >= 1; pages * page <= 2^31 - 1 */
+    int32_t page;      /* slots to a page: 16, 32, 64, ... 1024 */
+    int32_t h_kv, d;
+    int32_t dtype;     /* PBS_BF16, PBS_E4M3 or PBS_I8 */
+    void *K, *V;       /* [pages, h_kv, page, d] */
+    float *k_scale, *v_scale; /* [pages, h_kv, page] */
+} pbs_cache;
+
+/*
+ * Writes the rows of `tokens` tokens into the cache: K, V [tokens, h_kv, d] of `dtype` (PBS_BF16 or PBS_F32) with the given
+ * strides, slots [tokens] int32 in device memory.  A slot outside [0, pages * page) is passed over (the padding of a
+ * batch).  The slots of one call have to differ from each other; two tokens with the same slot leave an undefined row there.
+ * Every row that no slot names stays as it was.
+ * pbs_cache_read is the way back: row t of K, V [tokens, h_kv, d] of `dtype` becomes what slot slots[t] stands for
+ * (the held value times its factor in fp32, rounded to dtype), zeros for a slot outside the cache.  K or V may be NULL
+ * (then it is not read back); slots may repeat.
+ * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, page, too many slots or rows), PBS_ERR_HIP.
+ */
+pbs_status pbs_cache_write(const pbs_cache *c, int32_t dtype, int32_t tokens, const void *K, const pbs_strides *k,
+                           const void *V, const pbs_strides *v, const int32_t *slots, void *stream);
+pbs_status pbs_cache_read(const pbs_cache *c, int32_t dtype, int32_t tokens, const int32_t *slots, void *K,
+                          const pbs_strides *k, void *V, const pbs_strides *v, void *stream);
+
+/*
+ * Attention of each sequence's newest q_len tokens over its cached keys, a prefix that all sequences share in front of
+ * them: query t of sequence i sees all prefix_len prefix keys and its own keys 0 .. lens[i] - q_len + t (its own keys
+ * include the new tokens, written before this call).  O = softmax(scale * Q K^T) V over these; a query that sees none gets a
+ * zero row and lse = -inf.
+ *   Q, O     token i * q_len + t; dtype bf16 whatever the cache holds; h_q % c->h_kv == 0.  O may be Q itself.
+ *   page_table [n_seq, max_pages] int32: the pages of a sequence's own keys in order; entries behind its length are
+ *            not looked at.  A listed page outside [0, pages) counts as keys that nobody sees.
+ *   lens     [n_seq] int32, device memory: own keys; negative counts as 0, more than min(max_len, max_pages * page) as that.
+ *   max_len  an upper bound of lens that the host knows: it decides how the work is cut, not what comes out.
+ *   prefix_pages [ceil(prefix_len / page)] int32, device memory; NULL when prefix_len is 0.  The prefix is read once
+ *            for the whole batch, not once per sequence.
+ *   lse      [n_seq * q_len, h_q] float32 or NULL: log-sum-exp of the logits that each query sees.
+ *   ws       pbs_decode_workspace_bytes(p, c) bytes, 256-byte aligned (0: may be NULL); need not be initialised, means
+ *            nothing afterwards.  Calls that may overlap in time need one each.
+ * Probabilities enter the second product in bf16, everything else is fp32.
+ * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE (max_len or prefix_len negative, misaligned, a scale that is negative or not
+ * finite), PBS_ERR_UNSUPPORTED (q_len > 16, n_seq * q_len * h_q or n_seq * max_pages > 2^31 - 1 or a grid that is too large,
+ * dtype), PBS_ERR_WORKSPACE, PBS_ERR_HIP.
+ */
+typedef struct {
+    int32_t n_seq, q_len, h_q;
+    int32_t max_pages, max_len, prefix_len;
+    int32_t dtype;    /* of Q and O: PBS_BF16 */
+    float scale;      /* 0 means 1/sqrt(d) */
+    pbs_strides q, o;
+} pbs_decode_problem;
+size_t pbs_decode_workspace_bytes(const pbs_decode_problem *p, const pbs_cache *c);
+pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cache *c, const void *Q, const int32_t *page_table,
+                           const int32_t *lens, const int32_t *prefix_pages, void *O, float *lse, void *ws,
+                           size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

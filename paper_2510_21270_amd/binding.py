@@ -13,7 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpbs.so")
 _lib = None
 
-PBS_F32, PBS_BF16 = 0, 1
+PBS_F32, PBS_BF16, PBS_E4M3, PBS_I8 = 0, 1, 2, 3
 STAGE_KEY_SCORES, STAGE_SEGMENT_PERMUTE, STAGE_BLOCK_MASK, STAGE_ATTN_FWD, STAGE_UNPERMUTE = 1, 2, 3, 4, 5
 STAGE_QUERY_PERMUTE = 6
 FLAG_FORCE_FIRST_BLOCK, FLAG_TOKEN_ORDER_COPY, FLAG_RUNNING_MAX_ONLY, FLAG_KBAR_IN_WS, FLAG_INDEX_REMAP = 1, 2, 4, 8, 16
@@ -21,7 +21,9 @@ FLAG_FORCE_FIRST_BLOCK, FLAG_TOKEN_ORDER_COPY, FLAG_RUNNING_MAX_ONLY, FLAG_KBAR_
 EXPORTS = ["pbs_status_string", "pbs_validate", "pbs_workspace_bytes", "pbs_vt_bytes", "pbs_key_scores",
            "pbs_segment_permute", "pbs_permute_rows", "pbs_block_mask", "pbs_attn_fwd", "pbs_unpermute",
            "pbs_mfma_rate_probe", "pbs_key_scores_static", "pbs_key_scores_static_scratch_bytes", "pbs_admitted_lists",
-           "pbs_mass_covered", "pbs_key_scores_proxy", "pbs_query_permutation", "pbs_shader_clock_meter"]
+           "pbs_mass_covered", "pbs_key_scores_proxy", "pbs_query_permutation", "pbs_shader_clock_meter",
+           "pbs_rope", "pbs_rope_frequencies", "pbs_cache_write", "pbs_cache_read", "pbs_decode_workspace_bytes",
+           "pbs_decode_attn"]
 
 
 class PbsError(RuntimeError):
@@ -33,6 +35,29 @@ class pbs_problem(ctypes.Structure):
                 ("d", ctypes.c_int32), ("block", ctypes.c_int32), ("segment", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("tau", ctypes.c_float), ("scale", ctypes.c_float),
                 ("flags", ctypes.c_uint32)]
+
+
+class pbs_strides(ctypes.Structure):
+    _fields_ = [("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class pbs_rope_problem(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("h_q", ctypes.c_int32), ("h_kv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("rot", ctypes.c_int32), ("layout", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("flags", ctypes.c_uint32), ("q", pbs_strides), ("k", pbs_strides),
+                ("q_out", pbs_strides), ("k_out", pbs_strides)]
+
+
+class pbs_cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("h_kv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class pbs_decode_problem(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("q_len", ctypes.c_int32), ("h_q", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32), ("prefix_len", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("q", pbs_strides), ("o", pbs_strides)]
 
 
 def load_library():
@@ -66,6 +91,14 @@ def load_library():
         lib.pbs_mass_covered.argtypes = [P, V, V, V, V]
         lib.pbs_mfma_rate_probe.argtypes = [ctypes.c_int, ctypes.c_int, V, Z, ctypes.POINTER(ctypes.c_double), V]
         lib.pbs_shader_clock_meter.argtypes = [V, ctypes.c_int, V]
+        D, I, S, C = ctypes.c_double, ctypes.c_int32, ctypes.POINTER(pbs_strides), ctypes.POINTER(pbs_cache)
+        lib.pbs_rope.argtypes = [ctypes.POINTER(pbs_rope_problem), V, V, V, V, V, V, V]
+        lib.pbs_rope_frequencies.argtypes = [ctypes.c_int, I, D, D, D, D, D, ctypes.POINTER(D), ctypes.POINTER(D)]
+        lib.pbs_cache_write.argtypes = [C, I, I, V, S, V, S, V, V]
+        lib.pbs_cache_read.argtypes = [C, I, I, V, V, S, V, S, V]
+        lib.pbs_decode_workspace_bytes.restype = Z
+        lib.pbs_decode_workspace_bytes.argtypes = [ctypes.POINTER(pbs_decode_problem), C]
+        lib.pbs_decode_attn.argtypes = [ctypes.POINTER(pbs_decode_problem), C, V, V, V, V, V, V, V, Z, V]
         _lib = lib
     return _lib
 
@@ -307,6 +340,209 @@ def shader_clock_beside(fn, micros=20000, delay_s=0.02):
                "pbs_shader_clock_meter")
     torch.cuda.synchronize()
     return float(out[0]), float(out[1])
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Around the prefill path: tensors of [tokens, heads, d] with any token and head strides (a slice of a fused projection, a
+# transposed [heads, n, d] tensor).  The checks here are those that the library cannot make: sizes, types and devices of tensors.
+
+def _need(ok, what, why):
+    if not ok:
+        raise PbsError("%s: %s" % (what, why))
+
+
+def _device_of(what, *tensors):
+    """The device of all tensors given; they have to agree and to be on a GPU."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            _need(t.is_cuda, what, "a tensor is not on the GPU")
+            _need(dev is None or t.device == dev, what, "tensors on different devices")
+            dev = t.device
+    return dev
+
+
+def _launch(what, dev, fn, *args):
+    """fn(*args, stream) on the current stream of `dev`, whatever device is current."""
+    if dev.index == torch.cuda.current_device():
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    _check(st, what)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+_DTYPE_CODES = {torch.float32: PBS_F32, torch.bfloat16: PBS_BF16, torch.float8_e4m3fn: PBS_E4M3, torch.int8: PBS_I8}
+_NO_STRIDES = pbs_strides(0, 0)
+
+
+def _rows(what, x, name, d=None):
+    """Strides of a [tokens, heads, d] tensor whose features are consecutive."""
+    _need(x.dim() == 3 and (d is None or x.shape[2] == d), what, "%s has to be [tokens, heads, d]" % name)
+    st, sh, sd = x.stride()
+    _need(sd == 1 or x.numel() == 0, what, "the features of %s are not consecutive" % name)
+    return pbs_strides(st if x.shape[0] > 1 else 0, sh if x.shape[1] > 1 else 0)
+
+
+def _ints(what, x, name, *shape):
+    _need(x.dtype == torch.int32 and x.is_contiguous() and tuple(x.shape) == shape, what,
+          "%s has to be contiguous int32 of shape %s" % (name, list(shape)))
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {None: 0, "plain": 0, "linear": 1, "bands": 2, "ramp": 3}
+ROPE_TRANSPOSE = 1
+
+
+def rope_frequencies(rot, base=1e4, scaling=None, factor=1.0, original=4096, low=None, high=None, device="cuda"):
+    """(frequencies [rot / 2] float64 on `device`, magnitude) of rotary pairs, scaled for contexts longer than `original`:
+    None, "linear", "bands" (low, high: turns over the original context, 1 and 4) or "ramp" (1 and 32)."""
+    _need(scaling in ROPE_SCALINGS, "pbs_rope_frequencies", "unknown scaling %r" % (scaling,))
+    low = 1.0 if low is None else low
+    high = (32.0 if scaling == "ramp" else 4.0) if high is None else high
+    table, mag = (ctypes.c_double * max(1, rot // 2))(), ctypes.c_double(0.0)
+    _check(load_library().pbs_rope_frequencies(ROPE_SCALINGS[scaling], rot, base, factor, original, low, high, table,
+                                               ctypes.byref(mag)), "pbs_rope_frequencies")
+    return torch.tensor(list(table), dtype=torch.float64, device=device), mag.value
+
+
+def rope(Q, K, positions, freq, layout="half", magnitude=1.0, transpose=False, Qout=None, Kout=None):
+    """Q and K (either may be None) turned by their positions; new tensors, or in place with Qout=Q, Kout=K."""
+    what = "pbs_rope"
+    dev = _device_of(what, Q, K, positions, freq, Qout, Kout)
+    one = Q if Q is not None else K
+    _need(one is not None, what, "neither Q nor K")
+    _need(layout in ROPE_LAYOUTS, what, "unknown layout %r" % (layout,))
+    _need(magnitude != 0.0, what, "magnitude 0")
+    tokens, d = one.shape[0], one.shape[-1]
+    _ints(what, positions, "positions", tokens)
+    _need(freq.dtype == torch.float64 and freq.dim() == 1 and freq.is_contiguous(), what, "freq has to be contiguous float64")
+    if Q is not None and Qout is None:
+        Qout = torch.empty(Q.shape, dtype=Q.dtype, device=dev)
+    if K is not None and Kout is None:
+        Kout = torch.empty(K.shape, dtype=K.dtype, device=dev)
+    p = pbs_rope_problem(tokens, 0, 0, d, 2 * freq.shape[0], ROPE_LAYOUTS[layout], _DTYPE_CODES.get(one.dtype, -1),
+                         magnitude, ROPE_TRANSPOSE if transpose else 0)
+    for x, out, name in ((Q, Qout, "Q"), (K, Kout, "K")):
+        _need((x is None) == (out is None), what, "%sout without %s" % (name, name))
+        if x is None:
+            continue
+        _need(x.shape[0] == tokens and x.dtype == one.dtype and out.dtype == x.dtype and out.shape == x.shape, what,
+              "tensors of different sizes or types")
+        if name == "Q":
+            p.h_q, p.q, p.q_out = x.shape[1], _rows(what, x, name, d), _rows(what, out, "Qout", d)
+        else:
+            p.h_kv, p.k, p.k_out = x.shape[1], _rows(what, x, name, d), _rows(what, out, "Kout", d)
+    _launch(what, dev, load_library().pbs_rope, ctypes.byref(p), freq.data_ptr(), positions.data_ptr(), _addr(Q), _addr(K),
+            _addr(Qout), _addr(Kout))
+    return Qout, Kout
+
+
+class Cache:
+    """A paged key/value cache over K and V [pages, h_kv, page, d] (bf16, float8_e4m3fn or int8, the 8-bit ones with the
+    rows' factors k_scale and v_scale [pages, h_kv, page] float32)."""
+
+    def __init__(self, K, V, k_scale=None, v_scale=None):
+        what = "pbs_cache"
+        self.device = _device_of(what, K, V, k_scale, v_scale)
+        _need(K.dim() == 4 and K.shape == V.shape and K.dtype == V.dtype, what, "K and V have to be [pages, h_kv, page, d] alike")
+        _need(K.is_contiguous() and V.is_contiguous(), what, "pages have to be contiguous")
+        _need(K.dtype in _DTYPE_CODES and K.dtype != torch.float32, what, "a cache holds bf16, float8_e4m3fn or int8")
+        if K.dtype == torch.bfloat16:
+            k_scale = v_scale = None
+        else:
+            for f in (k_scale, v_scale):
+                _need(f is not None and f.dtype == torch.float32 and f.shape == K.shape[:3] and f.is_contiguous(), what,
+                      "factors have to be contiguous float32 [pages, h_kv, page]")
+        self.K, self.V, self.k_scale, self.v_scale = K, V, k_scale, v_scale
+        self.pages, self.h_kv, self.page, self.d = K.shape
+        self.c = pbs_cache(self.pages, self.page, self.h_kv, self.d, _DTYPE_CODES[K.dtype], K.data_ptr(), V.data_ptr(),
+                           _addr(k_scale), _addr(v_scale))
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def alloc(cls, pages, page, h_kv, d, dtype=torch.bfloat16, device="cuda"):
+        K = torch.zeros((pages, h_kv, page, d), dtype=torch.uint8 if dtype != torch.bfloat16 else dtype, device=device)
+        K, V = K.view(dtype), torch.zeros_like(K).view(dtype)
+        f = [None if dtype == torch.bfloat16 else torch.zeros((pages, h_kv, page), dtype=torch.float32, device=device)
+             for _ in range(2)]
+        return cls(K, V, *f)
+
+
+def cache_write(cache, K, V, slots):
+    """Rows K, V [tokens, h_kv, d] into the slots [tokens] of the cache; a slot outside it is passed over."""
+    what = "pbs_cache_write"
+    dev = _device_of(what, cache.K, K, V, slots)
+    _need(K.shape == V.shape and K.dtype == V.dtype and K.dim() == 3 and K.shape[1:] == (cache.h_kv, cache.d), what,
+          "K and V have to be [tokens, h_kv, d] alike")
+    _ints(what, slots, "slots", K.shape[0])
+    _launch(what, dev, load_library().pbs_cache_write, cache.ref, _DTYPE_CODES.get(K.dtype, -1), K.shape[0], K.data_ptr(),
+            _rows(what, K, "K"), V.data_ptr(), _rows(what, V, "V"), slots.data_ptr())
+
+
+def cache_read(cache, slots, dtype="bf16", K=None, V=None):
+    """(K, V) [tokens, h_kv, d] that the slots stand for; zeros for a slot outside the cache.  Into K and V where given."""
+    what = "pbs_cache_read"
+    dev = _device_of(what, cache.K, slots, K, V)
+    _ints(what, slots, "slots", slots.numel())
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}.get(dtype, dtype)
+    shape = (slots.numel(), cache.h_kv, cache.d)
+    out = [torch.empty(shape, dtype=dt, device=dev) if x is None else x for x in (K, V)]
+    for x in out:
+        _need(tuple(x.shape) == shape and x.dtype == dt, what, "K and V have to be [tokens, h_kv, d] of the type asked for")
+    _launch(what, dev, load_library().pbs_cache_read, cache.ref, _DTYPE_CODES.get(dt, -1), shape[0], slots.data_ptr(),
+            out[0].data_ptr(), _rows(what, out[0], "K"), out[1].data_ptr(), _rows(what, out[1], "V"))
+    return out[0], out[1]
+
+
+def _token_strides(what, x, name):
+    """Strides of a [n_seq, q_len, heads, d] tensor whose first two axes are one axis of tokens."""
+    s, t, h, e = x.stride()
+    _need(x.dim() == 4 and (e == 1 or x.numel() == 0), what, "the features of %s are not consecutive" % name)
+    _need(x.shape[0] <= 1 or x.shape[1] == 1 or s == x.shape[1] * t, what, "the tokens of %s are not evenly spaced" % name)
+    token = t if x.shape[1] > 1 else s if x.shape[0] > 1 else 0
+    return pbs_strides(token, h if x.shape[2] > 1 else 0)
+
+
+def decode_attn(cache, Q, page_table, lens, max_len=None, prefix_pages=None, prefix_len=0, scale=0.0, O=None, lse=None,
+                want_lse=False, ws=None):
+    """Attention of Q [n_seq, q_len, h_q, d], the newest tokens of n_seq sequences, over their cached keys: page_table
+    [n_seq, max_pages], lens [n_seq] own keys (the new ones among them, at most max_len), behind prefix_len keys of
+    prefix_pages that all sequences share.  O like Q; (O, lse [n_seq, q_len, h_q]) with want_lse."""
+    what = "pbs_decode_attn"
+    dev = _device_of(what, cache.K, Q, page_table, lens, prefix_pages, O, lse, ws)
+    _need(Q.dim() == 4 and Q.shape[3] == cache.d, what, "Q has to be [n_seq, q_len, h_q, d]")
+    n, q_len, h_q, d = Q.shape
+    _need(page_table.dim() == 2, what, "page_table has to be [n_seq, max_pages]")
+    _ints(what, page_table, "page_table", n, page_table.shape[1])
+    _ints(what, lens, "lens", n)
+    if prefix_len:
+        _need(prefix_pages is not None, what, "prefix_len without prefix_pages")
+        _ints(what, prefix_pages, "prefix_pages", prefix_pages.numel())
+        _need(prefix_pages.numel() >= -(-prefix_len // cache.page), what, "prefix_pages is shorter than prefix_len")
+    if max_len is None:
+        max_len = page_table.shape[1] * cache.page
+    if O is None:
+        O = torch.empty(Q.shape, dtype=Q.dtype, device=dev)
+    _need(O.shape == Q.shape and O.dtype == Q.dtype, what, "O has to be like Q")
+    if lse is None and want_lse:
+        lse = torch.empty((n, q_len, h_q), dtype=torch.float32, device=dev)
+    if lse is not None:
+        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (n, q_len, h_q), what,
+              "lse has to be contiguous float32 [n_seq, q_len, h_q]")
+    p = pbs_decode_problem(n, q_len, h_q, page_table.shape[1], max_len, prefix_len, _DTYPE_CODES.get(Q.dtype, -1), scale,
+                           _token_strides(what, Q, "Q"), _token_strides(what, O, "O"))
+    ref, lib = ctypes.byref(p), load_library()
+    need = lib.pbs_decode_workspace_bytes(ref, cache.ref)
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _launch(what, dev, lib.pbs_decode_attn, ref, cache.ref, Q.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
+            _addr(prefix_pages), O.data_ptr(), _addr(lse), _addr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    return (O, lse) if lse is not None else O
 
 
 class Pipeline:
