@@ -306,8 +306,8 @@ pbs_status pbs_shader_clock_meter(float *out, int micros, void *stream);
 
 /*
  * ---------------------------------------------------------------------------------------------------------------
- * Around the prefill path: rotary positions in front of it, the paged key/value cache behind it, and attention of new
- * tokens over that cache.
+ * Around the prefill path: rotary positions in front of it, the paged key/value cache behind it, attention of new
+ * tokens over that cache, and causal attention over packed prompts that are too short for block selection to pay.
  *
  * These calls see tensors as tokens x heads x features: element (t, h, e) of a tensor lies at t * strides.token +
  * h * strides.head + e, in elements; features are consecutive.  [tokens, heads, d] memory has strides {heads * d, d}, the
@@ -428,6 +428,31 @@ size_t pbs_decode_workspace_bytes(const pbs_decode_problem *p, const pbs_cache *
 pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cache *c, const void *Q, const int32_t *page_table,
                            const int32_t *lens, const int32_t *prefix_pages, void *O, float *lse, void *ws,
                            size_t ws_bytes, void *stream);
+
+/*
+ * Attention over prompts packed one behind the other.  Sequence i has the query rows cu_q[i] .. cu_q[i+1] - 1 and the key
+ * rows cu_k[i] .. cu_k[i+1] - 1 (cu_q, cu_k [n_seq + 1] int32, device memory, ascending; a place outside [0, total_q] or
+ * [0, total_k] is taken as the nearest inside, a length below zero as zero).  With PBS_PROMPT_CAUSAL query t of a sequence sees
+ * key j iff j <= t + (number of keys) - (number of queries): the newest query sees everything, as when a chunk of a
+ * prompt follows keys that are there already; without it every query sees every key of its sequence.  A query that sees no
+ * key gets a zero row and lse = -inf.  Rows of O and lse that belong to no sequence stay as they were.
+ *   Q, O [total_q, h_q, d], K, V [total_k, h_kv, d], bf16; h_q % h_kv == 0, h_q / h_kv <= 128; lse [total_q, h_q] float32 or NULL.
+ *   O may not overlap Q, K or V.
+ * Probabilities enter the second product in bf16, everything else is fp32.
+ * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, h_q / h_kv > 128, rows beyond 2^31 - 1, a grid that is
+ * too large, K or V of one head spanning 2 GiB or more), PBS_ERR_HIP.
+ */
+enum { PBS_PROMPT_CAUSAL = 1u };
+typedef struct {
+    int32_t n_seq, total_q, total_k;
+    int32_t h_q, h_kv, d;
+    int32_t dtype;    /* PBS_BF16 */
+    float scale;      /* 0 means 1/sqrt(d) */
+    uint32_t flags;   /* PBS_PROMPT_CAUSAL */
+    pbs_strides q, k, v, o;
+} pbs_prompt_problem;
+pbs_status pbs_prompt_attn(const pbs_prompt_problem *p, const void *Q, const void *K, const void *V, const int32_t *cu_q,
+                           const int32_t *cu_k, void *O, float *lse, void *stream);
 
 #ifdef __cplusplus
 }

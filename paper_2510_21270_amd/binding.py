@@ -23,7 +23,7 @@ EXPORTS = ["pbs_status_string", "pbs_validate", "pbs_workspace_bytes", "pbs_vt_b
            "pbs_mfma_rate_probe", "pbs_key_scores_static", "pbs_key_scores_static_scratch_bytes", "pbs_admitted_lists",
            "pbs_mass_covered", "pbs_key_scores_proxy", "pbs_query_permutation", "pbs_shader_clock_meter",
            "pbs_rope", "pbs_rope_frequencies", "pbs_cache_write", "pbs_cache_read", "pbs_decode_workspace_bytes",
-           "pbs_decode_attn"]
+           "pbs_decode_attn", "pbs_prompt_attn"]
 
 
 class PbsError(RuntimeError):
@@ -58,6 +58,13 @@ class pbs_decode_problem(ctypes.Structure):
     _fields_ = [("n_seq", ctypes.c_int32), ("q_len", ctypes.c_int32), ("h_q", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32), ("prefix_len", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("q", pbs_strides), ("o", pbs_strides)]
+
+
+class pbs_prompt_problem(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("total_q", ctypes.c_int32), ("total_k", ctypes.c_int32),
+                ("h_q", ctypes.c_int32), ("h_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("flags", ctypes.c_uint32), ("q", pbs_strides), ("k", pbs_strides),
+                ("v", pbs_strides), ("o", pbs_strides)]
 
 
 def load_library():
@@ -99,6 +106,7 @@ def load_library():
         lib.pbs_decode_workspace_bytes.restype = Z
         lib.pbs_decode_workspace_bytes.argtypes = [ctypes.POINTER(pbs_decode_problem), C]
         lib.pbs_decode_attn.argtypes = [ctypes.POINTER(pbs_decode_problem), C, V, V, V, V, V, V, V, Z, V]
+        lib.pbs_prompt_attn.argtypes = [ctypes.POINTER(pbs_prompt_problem), V, V, V, V, V, V, V, V]
         _lib = lib
     return _lib
 
@@ -542,6 +550,41 @@ def decode_attn(cache, Q, page_table, lens, max_len=None, prefix_pages=None, pre
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _launch(what, dev, lib.pbs_decode_attn, ref, cache.ref, Q.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
             _addr(prefix_pages), O.data_ptr(), _addr(lse), _addr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    return (O, lse) if lse is not None else O
+
+
+PROMPT_CAUSAL = 1
+
+
+def prompt_attn(Q, K, V, cu_q, cu_k=None, causal=True, scale=0.0, O=None, lse=None, want_lse=False):
+    """Attention of packed prompts: Q [total_q, h_q, d] over K, V [total_k, h_kv, d], sequence i being the rows cu_q[i] ..
+    cu_q[i + 1] - 1 and cu_k[i] .. cu_k[i + 1] - 1 (cu_q where cu_k is None).  Causal: the last query sees the last key.
+    O like Q, its rows of no sequence as they were (new memory is not cleared); (O, lse [total_q, h_q]) with want_lse."""
+    what = "pbs_prompt_attn"
+    dev = _device_of(what, Q, K, V, cu_q, cu_k, O, lse)
+    _need(Q.dim() == 3 and K.dim() == 3 and K.shape == V.shape and K.shape[2] == Q.shape[2], what,
+          "Q, K and V have to be [rows, heads, d], K and V alike")
+    _need(Q.dtype == K.dtype == V.dtype, what, "tensors of different types")
+    total, h_q, d = Q.shape
+    if cu_k is None:
+        cu_k = cu_q
+        _need(K.shape[0] == total, what, "without cu_k there is a key to every query")
+    _need(cu_q.dim() == 1 and cu_q.numel() >= 1, what, "cu_q has to be [n_seq + 1]")
+    _ints(what, cu_q, "cu_q", cu_q.numel())
+    _ints(what, cu_k, "cu_k", cu_q.numel())
+    if O is None:
+        O = torch.empty(Q.shape, dtype=Q.dtype, device=dev)
+    _need(O.shape == Q.shape and O.dtype == Q.dtype, what, "O has to be like Q")
+    if lse is None and want_lse:
+        lse = torch.empty((total, h_q), dtype=torch.float32, device=dev)
+    if lse is not None:
+        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (total, h_q), what,
+              "lse has to be contiguous float32 [total_q, h_q]")
+    p = pbs_prompt_problem(cu_q.numel() - 1, total, K.shape[0], h_q, K.shape[1], d, _DTYPE_CODES.get(Q.dtype, -1), scale,
+                           PROMPT_CAUSAL if causal else 0, _rows(what, Q, "Q"), _rows(what, K, "K"), _rows(what, V, "V"),
+                           _rows(what, O, "O"))
+    _launch(what, dev, load_library().pbs_prompt_attn, ctypes.byref(p), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+            cu_q.data_ptr(), cu_k.data_ptr(), O.data_ptr(), _addr(lse))
     return (O, lse) if lse is not None else O
 
 

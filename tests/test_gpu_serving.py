@@ -407,3 +407,164 @@ def test_decode_on_another_stream_and_captured():
         got = O.clone()
         eager = pbs.decode_attn(s.cache, Q, table, lens, prefix_pages=pre, prefix_len=s.prefix)
         assert torch.equal(got, eager)
+
+
+# ------------------------------------------------------------------------------------------------ prompts
+def _cu(lens):
+    return torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32)
+
+
+def _prompts(seed, lens, before, h_q, h_kv, d):
+    keys = [n + b for n, b in zip(lens, before)]
+    Q = (1.5 * _randn(seed, sum(lens), h_q, d)).bfloat16()
+    K, V = _randn(seed + 1, sum(keys), h_kv, d).bfloat16(), (2 * _randn(seed + 2, sum(keys), h_kv, d)).bfloat16()
+    return Q, K, V, _cu(lens), _cu(keys)
+
+
+def _check_prompts(Q, K, V, cu_q, cu_k, O, lse, causal=True, scale=None, rows=None):
+    r, d = Q.shape[1] // K.shape[1], Q.shape[2]
+    for i in range(cu_q.numel() - 1):
+        q0, q1, k0, k1 = int(cu_q[i]), int(cu_q[i + 1]), int(cu_k[i]), int(cu_k[i + 1])
+        t = torch.arange(q1 - q0) if rows is None else torch.tensor([x for x in rows if x < q1 - q0], dtype=torch.int64)
+        if t.numel() == 0:
+            continue
+        sees = torch.arange(k1 - k0)[None] <= t[:, None] + (k1 - k0) - (q1 - q0)
+        if not causal:
+            sees = torch.ones_like(sees)
+        for h in range(Q.shape[1]):
+            o, l, bo, bl = attention_ref(Q[q0 + t, h], K[k0:k1, h // r], V[k0:k1, h // r], sees, scale or 1 / math.sqrt(d))
+            within(O[q0 + t, h], o, bo, "O of sequence %d, head %d" % (i, h))
+            if lse is not None:
+                within(lse[q0 + t, h], l, bl, "lse of sequence %d, head %d" % (i, h))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("h_q,h_kv,d", [(4, 1, 128), (8, 2, 64), (7, 1, 128), (3, 3, 64), (2, 2, 128)])
+def test_prompt_lengths(h_q, h_kv, d, causal):
+    lens = [1, 0, 2, 15, 17, 31, 32, 33, 0, 64, 65, 130, 1]
+    Q, K, V, cu, _ = _prompts(20, lens, [0] * len(lens), h_q, h_kv, d)
+    O, lse = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda(), causal=causal, want_lse=True)
+    _check_prompts(Q, K, V, cu, cu, O, lse, causal)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("h_q,h_kv,d", [(8, 2, 128), (5, 1, 64), (128, 1, 64), (96, 1, 128)])
+def test_prompt_chunks_behind_keys_and_queries_that_see_none(h_q, h_kv, d, causal):
+    lens, before = [3, 40, 1, 20, 7, 33, 5], [500, 1, 64, -8, -7, 31, -5]
+    if h_q > 20:
+        lens, before = lens[:5], [100, 1, 64, -8, -7]
+    Q, K, V, cu_q, cu_k = _prompts(21, lens, before, h_q, h_kv, d)
+    O, lse = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu_q.cuda(), cu_k.cuda(), causal=causal, want_lse=True)
+    _check_prompts(Q, K, V, cu_q, cu_k, O, lse, causal)
+    if causal:
+        a = int(cu_q[3])
+        assert float(O[a:a + 8].abs().max()) == 0.0 and bool((lse[a:a + 8] == -math.inf).all())
+
+
+@pytest.mark.parametrize("h_q,h_kv,d", [(4, 1, 128), (2, 2, 128), (4, 2, 64)])
+def test_prompt_long(h_q, h_kv, d):
+    Q, K, V, cu_q, cu_k = _prompts(22, [2050, 700], [0, 1333], h_q, h_kv, d)
+    O, lse = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu_q.cuda(), cu_k.cuda(), want_lse=True)
+    _check_prompts(Q, K, V, cu_q, cu_k, O, lse, rows=[0, 1, 31, 32, 33, 127, 128, 255, 256, 511, 699, 1000, 1024, 2047, 2048, 2049])
+    again, lse2 = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu_q.cuda(), cu_k.cuda(), want_lse=True)
+    assert torch.equal(O, again) and torch.equal(lse, lse2)
+
+
+def test_prompt_many_sequences():
+    lens = [(7 * i) % 23 for i in range(200)]
+    Q, K, V, cu, _ = _prompts(23, lens, [0] * 200, 4, 2, 64)
+    O, lse = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda(), want_lse=True)
+    _check_prompts(Q, K, V, cu, cu, O, lse)
+
+
+def test_prompt_rows_of_no_sequence_stay_as_they_were():
+    Q, K, V, cu_q, cu_k = _prompts(24, [5, 30, 10], [0, 0, 0], 4, 2, 128)
+    O = torch.full((45, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((45, 4), 9.0, device="cuda")
+    part = torch.tensor([2, 5, 35], dtype=torch.int32)     # rows 0, 1 and 35 .. belong to none
+    pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), part.cuda(), part.cuda(), O=O, lse=lse)
+    assert bool((O[:2] == 7).all()) and bool((O[35:] == 7).all()) and bool((lse[:2] == 9).all()) and bool((lse[35:] == 9).all())
+    _check_prompts(Q, K, V, part, part, O, lse)
+    # places outside the tensors are taken as the nearest inside
+    wild = torch.tensor([-4, 5, 1000], dtype=torch.int32)
+    got = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), wild.cuda())
+    tame = torch.tensor([0, 5, 45], dtype=torch.int32)
+    assert torch.equal(got, pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), tame.cuda()))
+
+
+def test_prompt_strided():
+    Q, K, V, cu, _ = _prompts(25, [50, 83], [0, 0], 8, 2, 64)
+    want = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda())
+    fused = torch.cat((Q, K, V), 1).cuda()                 # a fused projection
+    O = torch.zeros(8, 133, 64, dtype=torch.bfloat16, device="cuda")           # [heads, n, d]
+    pbs.prompt_attn(fused[:, :8], fused[:, 8:10], fused[:, 10:], cu.cuda(), O=O.transpose(0, 1))
+    assert torch.equal(O.transpose(0, 1), want)
+    heads = [x.transpose(0, 1).contiguous().cuda().transpose(0, 1) for x in (Q, K, V)]
+    assert torch.equal(pbs.prompt_attn(*heads, cu.cuda()), want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_values_that_are_not_finite(d):
+    # keys 40 and 100 hold infinities and NaN: queries in front of them do not see it, nor does the next sequence
+    Q, K, V, cu, _ = _prompts(26, [130, 64], [0, 0], 4, 1, d)
+    V[40, 0, 3], V[40, 0, 4], V[100, 0, 5], V[100, 0, 6] = math.inf, -math.inf, math.nan, math.inf
+    V[41, 0, 4] = math.inf
+    O, lse = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda(), want_lse=True)
+    got = O.float().cpu()
+    assert torch.isfinite(got[:40]).all() and torch.isfinite(got[130:]).all()
+    assert (got[40:130, :, 3] == math.inf).all() and (got[40, :, 4] == -math.inf).all() and torch.isnan(got[41:130, :, 4]).all()
+    assert torch.isfinite(got[40:100, :, 5:]).all() and torch.isnan(got[100:130, :, 5]).all() and (got[100:130, :, 6] == math.inf).all()
+    clean = [i for i in range(d) if i not in (3, 4, 5, 6)]
+    V.nan_to_num_(0.0, 0.0, 0.0)
+    ref, lse2 = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda(), want_lse=True)
+    assert torch.equal(ref[..., clean], O[..., clean]) and torch.equal(lse, lse2)
+    _check_prompts(Q, K, V, cu, cu, ref, lse2)
+
+
+def test_prompt_logits_that_are_not_finite():
+    Q, K, V, cu, _ = _prompts(27, [70, 40], [0, 0], 4, 2, 64)
+    K[50, 1] = math.nan                                    # kv head 1: heads 2 and 3 from query 50 on
+    Q[5, 0, 0] = math.nan
+    Q[100, 3, 0] = math.inf
+    O, lse = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda(), want_lse=True)
+    bad = torch.zeros(110, 4, dtype=torch.bool)
+    bad[50:70, 2:] = bad[5, 0] = bad[100, 3] = True
+    got, l = O.float().cpu(), lse.cpu()
+    assert torch.isnan(got[bad]).all() and torch.isfinite(got[~bad]).all() and torch.isfinite(l[~bad]).all() and torch.isnan(l[bad]).all()
+
+
+def test_prompt_logits_that_grow_along_the_keys():
+    # each tile's maximum far above the one before: hundreds of nats from the first key to the last, in steps and in one leap
+    n, d = 600, 128
+    Q, K, V, cu, _ = _prompts(28, [n], [0], 2, 1, d)
+    Q = Q * 0.2
+    for shape in ("steps", "leap", "fall"):
+        u = torch.zeros(d)
+        u[0] = 1.0
+        Q[:, :, 0] = 8.0
+        k = K.clone()
+        ramp = torch.arange(n).float() * 0.5
+        k[:, 0, 0] = {"steps": ramp, "leap": (torch.arange(n) >= 300).float() * 400, "fall": 300 - ramp}[shape].bfloat16()
+        O, lse = pbs.prompt_attn(Q.cuda(), k.cuda(), V.cuda(), cu.cuda(), want_lse=True)
+        _check_prompts(Q, k, V, cu, cu, O, lse, rows=[0, 31, 32, 64, 100, 299, 300, 301, 320, 500, 599])
+
+
+def test_prompt_on_another_stream_and_captured():
+    Q, K, V, cu, _ = [x.cuda() for x in _prompts(29, [300, 20, 77], [0, 0, 0], 8, 2, 128)]
+    O = torch.zeros_like(Q)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        pbs.prompt_attn(Q, K, V, cu, O=O)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(O, pbs.prompt_attn(Q, K, V, cu))
+    with torch.cuda.graph(graph):
+        pbs.prompt_attn(Q, K, V, cu, O=O)
+    for k in range(3):                                     # other inputs and other lengths in the same memory
+        V.mul_(1.5)
+        cu.copy_(torch.tensor([0, 300 - 50 * k, 320, 397], dtype=torch.int32))
+        O.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(O, pbs.prompt_attn(Q, K, V, cu))

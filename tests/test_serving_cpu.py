@@ -187,3 +187,34 @@ def test_the_binding_refuses_what_the_library_cannot_see():
         b.rope_frequencies(64, scaling="other", device="cpu")
     f, mag = b.rope_frequencies(64, 1e4, device="cpu")
     assert f.shape == (32,) and f.dtype == torch.float64 and mag == 1.0
+
+
+def test_prompt_refusals(lib):
+    def prob(**kw):
+        x = dict(n_seq=2, total_q=10, total_k=12, h_q=4, h_kv=2, d=64, dtype=1, scale=0.0, flags=1)
+        x.update(kw)
+        p = b.pbs_prompt_problem(**x)
+        p.q = p.o = b.pbs_strides(256, 64)
+        p.k = p.v = b.pbs_strides(128, 64)
+        return p
+
+    def call(p=None, Q=FAKE, K=FAKE, V=FAKE, cu_q=FAKE, cu_k=FAKE, O=FAKE, lse=None):
+        return lib.pbs_prompt_attn(ctypes.byref(prob() if p is None else p), Q, K, V, cu_q, cu_k, O, lse, None)
+
+    assert lib.pbs_prompt_attn(None, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, None) == 1
+    for name in ("Q", "K", "V", "cu_q", "cu_k", "O"):
+        assert call(**{name: None}) == 1, name
+    assert call(prob(n_seq=0), Q=None) == 0 and call(prob(total_q=0), O=None) == 0
+    for kw in (dict(n_seq=-1), dict(total_q=-1), dict(total_k=-1), dict(h_q=0), dict(h_q=3), dict(h_kv=0), dict(scale=-0.5),
+               dict(scale=math.nan), dict(scale=math.inf)):
+        assert call(prob(**kw)) == 2, kw
+    for kw in (dict(dtype=0), dict(dtype=2), dict(d=96), dict(h_q=258, h_kv=2), dict(total_q=2 ** 30), dict(total_k=2 ** 23),
+               dict(total_k=2 ** 31 - 1, h_q=1, h_kv=1)):
+        assert call(prob(**kw)) == 3, kw
+    assert call(Q=ODD) == 2 and call(V=ODD) == 2 and call(O=ODD) == 2 and call(lse=ctypes.c_void_p(4098)) == 2
+    p = prob()
+    p.o = b.pbs_strides(64, 64)
+    assert call(p) == 2
+    p = prob()
+    p.k = b.pbs_strides(130, 64)
+    assert call(p) == 2
