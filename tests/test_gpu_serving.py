@@ -517,8 +517,12 @@ def test_prompt_values_that_are_not_finite(d):
     clean = [i for i in range(d) if i not in (3, 4, 5, 6)]
     V.nan_to_num_(0.0, 0.0, 0.0)
     ref, lse2 = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda(), want_lse=True)
-    assert torch.equal(ref[..., clean], O[..., clean]) and torch.equal(lse, lse2)
     _check_prompts(Q, K, V, cu, cu, ref, lse2)
+    # the other features: keys in tiles with such values are summed relative to another maximum than without, p e^(m - m') for
+    # p, so that roundings differ; either is within the bound, each weight's rounding being relative to the weight
+    mixed = ref.clone()
+    mixed[..., clean] = O[..., clean]
+    _check_prompts(Q, K, V, cu, cu, mixed, lse)
 
 
 def test_prompt_logits_that_are_not_finite():
