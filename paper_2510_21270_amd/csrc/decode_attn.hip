@@ -10,9 +10,13 @@
 // of the one it multiplies.  8-bit values become bf16 exactly; a key's factor is applied to its logit, a value row's
 // to its probability.
 //
-// The bytes of the cache bound it.  A call has few queries, so each (sequence, kv head) is cut into parts of the key axis that
-// leave O^T, m and l in the workspace, and a second launch joins them.  The prefix is cut in the same way, but its rows are the
-// queries of the whole batch: its keys are read once.
+// The bytes of the cache bound it, and a batch's lengths differ by orders of magnitude, known to the device alone.  The tiles of
+// all (sequence, kv head) units lie one behind the other in thought, and every wave takes an equal share of that row of
+// tiles: the end of one unit, a few whole ones, the start of the next.  A piece of a unit leaves O^T, m and l in the
+// workspace and a second launch joins the pieces; a unit that lies in one share whole is stored at once.  The prefix is
+// cut into parts of its keys, and its rows are the queries of the whole batch: its keys are read once.
+#include <type_traits>
+
 #include "pbs_host.h"
 #include "serving.h"
 
@@ -21,14 +25,19 @@ namespace pbs {
 constexpr int kDecWaves = 4;
 constexpr int kDecThreads = 64 * kDecWaves;
 constexpr int kTileKeys = 32;
-constexpr int kMostChunk = 4096;                           // keys of a part: a wave's pages fit its 64 lanes
+constexpr int kMostChunk = 4096;                           // keys of a part of the prefix
+constexpr int kHeldTiles = 32;                             // tiles whose pages (two each) a wave's lanes hold
+constexpr int kWholeKeys = 128;                            // lengths up to which a unit has a wave to itself
+constexpr int kUnitCost = 2;                               // tiles
 constexpr int kMostQueries = 16;
 
 struct DecodeArgs {
     int n_seq, q_len, h_q, h_kv, r;
     int page_log, pages, max_pages, max_len, prefix_len;
-    int chunk, parts;                                      // keys of a part (own keys), most parts of a sequence
     int row_tiles;                                         // of a sequence's q_len * r rows
+    int units;                                             // of a sequence: h_kv * row_tiles
+    int shares;                                            // waves of the own keys
+    int slot_rows;                                         // rows of a piece in the workspace
     int p_chunk, p_parts, p_row_tiles;                     // the same of the prefix
     float c2;                                              // scale * log2(e)
     pbs_strides q, o;
@@ -37,7 +46,8 @@ struct DecodeArgs {
     const float *kf, *vf;
     const int32_t *table, *lens, *prefix;
     bf16_t *O;
-    float *lse, *part_o, *part_ml;
+    float *lse, *part_o, *part_ml, *piece_o, *piece_ml;
+    int2 *pieces;                                          // of a unit: its first slot and how many
 };
 
 // own keys of sequence i
@@ -116,34 +126,19 @@ struct DecodeState {
     float m[NT], l[NT];                                    // m in log2 units, the same in a query's four lanes; l: this lane's keys
 };
 
-// V^T with the values that are not finite taken out, and where they were.
-__device__ __forceinline__ bool not_finite(uint32_t pair)
+// the pair without what is not finite
+__device__ __forceinline__ uint32_t finite_part(uint32_t pair)
 {
-    return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
-}
-// kind 0: finite values, 1: +inf, 2: -inf, 3: NaN; the latter three as ones
-__device__ __forceinline__ uint32_t pick_kind(uint32_t pair, int kind)
-{
-    uint32_t out = 0;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const uint32_t v = (pair >> (16 * x)) & 0xffffu;
-        const bool odd = (v & 0x7f80u) == 0x7f80u, inf = (v & 0x7fffu) == 0x7f80u;
-        uint32_t w = 0;
-        if (kind == 0) w = odd ? 0u : v;
-        else if (kind == 1) w = inf && v < 0x8000u ? 0x3f80u : 0u;
-        else if (kind == 2) w = inf && v >= 0x8000u ? 0x3f80u : 0u;
-        else w = odd && !inf ? 0x3f80u : 0u;
-        out |= w << (16 * x);
-    }
-    return out;
+    const uint32_t lo = (pair & 0x7f80u) == 0x7f80u ? 0u : pair & 0xffffu, hi = (pair & 0x7f800000u) == 0x7f800000u ? 0u : pair & 0xffff0000u;
+    return lo | hi;
 }
 
-// One tile of 32 keys, the first of them key0.  `sees[nt]`: keys below it are visible to the lane's query; `all`: keys
-// below it are visible to every query of the wave, keys at or above `none` to no query.
-template <int DTYPE, int D, int NT>
+// One tile of 32 keys, the first of them key0.  Keys below sees[nt] are visible to the lane's query, keys below `all` to every
+// query of the call, keys at or above `none` to no query.  SEVERAL: sees differs between queries; what is not finite in rows
+// that some of them see is left out (a hidden row's weight is zero, but 0 * inf is NaN), and `dropped` says so.
+template <int DTYPE, int D, int NT, bool SEVERAL>
 __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile32<DTYPE, D> &t, const bf16x8 (&q)[D / 32][NT],
-                                              const int (&sees)[NT], int key0, int all, int none, float c2, int g)
+                                              const int (&sees)[NT], int key0, int all, int none, float c2, int g, bool &dropped)
 {
     constexpr int NJ = D / 16;
     floatx4 s[2][NT];
@@ -170,7 +165,7 @@ __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             y[e] = s[e >> 2][nt][e & 3] * (DTYPE == PBS_BF16 ? c2 : t.kf[e >> 2][e & 3] * c2);
-            if (masked && !(t.ok[e >> 2] && key0 + 16 * (e >> 2) + 4 * g + (e & 3) < sees[nt])) y[e] = -INFINITY;
+            if (masked && !(t.ok[e >> 2] && key0 + 16 * (e >> 2) + 4 * g + (e & 3) < (SEVERAL ? sees[nt] : none))) y[e] = -INFINITY;
             top = fmaxf(top, y[e]);
         }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -219,51 +214,20 @@ __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile
 #pragma unroll
             for (int x = 0; x < NJ / 2; ++x) w[e][x] = 0;
         }
+        if (SEVERAL && masked && key0 + 16 * (e >> 2) + 4 * g + (e & 3) >= all) {
+#pragma unroll
+            for (int x = 0; x < NJ / 2; ++x) {
+                const uint32_t f = finite_part(w[e][x]);
+                dropped = dropped || f != w[e][x];
+                w[e][x] = f;
+            }
+        }
     }
     auto turned = [&](int j) {                             // feature j of the lane's: its eight keys
         const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
         return uintx4{__builtin_amdgcn_perm(w[1][j >> 1], w[0][j >> 1], sel), __builtin_amdgcn_perm(w[3][j >> 1], w[2][j >> 1], sel),
                       __builtin_amdgcn_perm(w[5][j >> 1], w[4][j >> 1], sel), __builtin_amdgcn_perm(w[7][j >> 1], w[6][j >> 1], sel)};
     };
-    bool odd = false;                                      // some query does not see a row that another does, with inf or NaN
-    if (masked && all < none) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int x = 0; x < NJ / 2; ++x) odd = odd || not_finite(w[e][x]);
-    }
-    if (__any(odd)) {
-        // finite values by their probabilities; of the others only which kind a query sees counts
-        const bf16_t one = (bf16_t)1.0f, zero = (bf16_t)0.0f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const uintx4 v = turned(j);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                bf16x8 seen;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    seen[e] = t.ok[e >> 2] && key0 + 16 * (e >> 2) + 4 * g + (e & 3) < sees[nt] ? one : zero;
-#pragma unroll
-                for (int kind = 0; kind < 4; ++kind) {
-                    uintx4 k;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) k[x] = pick_kind(v[x], kind);
-                    const bf16x8 ka = __builtin_bit_cast(bf16x8, k);
-                    if (kind == 0) {
-                        st.o[j][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, p[nt], st.o[j][nt], 0, 0, 0);
-                    } else {
-                        const floatx4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, seen, floatx4{0}, 0, 0, 0);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (n[i] > 0.0f)
-                                st.o[j][nt][i] += kind == 1 ? INFINITY : kind == 2 ? -INFINITY : __uint_as_float(0x7fc00000u);
-                    }
-                }
-            }
-        }
-        return;
-    }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
         const bf16x8 va = __builtin_bit_cast(bf16x8, turned(j));
@@ -273,83 +237,265 @@ __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile
     }
 }
 
-// Rows row0 .. row0 + 16 NT - 1 of `rows` (row x: token token0 + x / r, head h * r + x % r) against keys begin .. end - 1 of the
-// list `table` (len keys), left in part `part` of the workspace, or in O where the call has a single part.
+// What a wave does: rows row0 .. row0 + 16 NT - 1 of `rows` (row x: token token0 + x / r, head h * r + x % r) against tiles first,
+// first + STEP, ... of keys 0 .. end - 1 of the list `table` (of len keys).
+template <int DTYPE, int D, int NT, bool SEVERAL, bool OWN, int STEP>
+__device__ __forceinline__ void walk_keys(DecodeState<D, NT> &st, const DecodeArgs &a, const int32_t *table, int len, int first,
+                                          int end, int token0, int rows, int row0, int h)
+{
+    constexpr int NJ = D / 16;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    // lane x holds the page of 16 keys x of this wave's tiles
+    const int tiles = ceil_div(end, kTileKeys);
+    const int mine = tiles > first ? (tiles - first + STEP - 1) / STEP : 0;
+    int held = -1;
+    auto hold = [&](int from) __attribute__((always_inline)) {
+        const int it = from + (lane >> 1), key = (first + STEP * it) * kTileKeys + 16 * (lane & 1);
+        held = -1;
+        if (it < mine && key < end) {
+            held = table[key >> a.page_log];
+            if (held >= a.pages) held = -1;
+        }
+    };
+    auto fetch = [&](Tile32<DTYPE, D> &t, int it) __attribute__((always_inline)) {
+        const int key0 = (first + STEP * it) * kTileKeys, at = 2 * (it & (kHeldTiles - 1));
+        const int page[2] = {__builtin_amdgcn_readlane(held, at), __builtin_amdgcn_readlane(held, at + 1)};
+        const int in_page = (1 << a.page_log) - 1;
+        const int place[2] = {key0 & in_page, (key0 + 16) & in_page};
+        load_tile<DTYPE, D>(t, a, page, place, h, c, g);
+    };
+    hold(0);
+    bf16x8 q[D / 32][NT];
+    int sees[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int rc = min(row0 + 16 * nt + c, rows - 1), t = rc / a.r;
+        const bf16_t *src = a.Q + (int64_t)(token0 + t) * a.q.token + (int64_t)(h * a.r + rc - t * a.r) * a.q.head;
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x)
+            q[x][nt] = *reinterpret_cast<const bf16x8 *>(src + (DTYPE == PBS_BF16 ? 32 * x + 8 * g : 64 * (x >> 1) + 16 * g + 8 * (x & 1)));
+        sees[nt] = OWN ? len - a.q_len + t + 1 : len;
+        st.m[nt] = -INFINITY;
+        st.l[nt] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) st.o[j][nt] = floatx4{0};
+    }
+    const int all = OWN ? len - a.q_len + 1 : len;
+
+    Tile32<DTYPE, D> ta, tb;
+    bool dropped = false;
+    auto use = [&](const Tile32<DTYPE, D> &t, int it) __attribute__((always_inline)) {
+        multiply_tile<DTYPE, D, NT, SEVERAL>(st, t, q, sees, (first + STEP * it) * kTileKeys, all, len, a.c2, g, dropped);
+    };
+    if (mine > 0) fetch(ta, 0);
+    for (int it = 0; it < mine; it += 2) {
+        if (it + 1 < mine) fetch(tb, it + 1);
+        use(ta, it);
+        if (it + 1 < mine) {
+            if (it + 2 < mine) {
+                if (((it + 2) & (kHeldTiles - 1)) == 0) hold(it + 2);
+                fetch(ta, it + 2);
+            }
+            use(tb, it + 1);
+        }
+    }
+    if constexpr (SEVERAL && DTYPE != PBS_I8) {
+        // what was left out, for the queries that see it: infinities and NaN come through any weight
+        if (__builtin_expect(__any(dropped), 0)) {
+            for (int key = max(all, first * kTileKeys); key < end; ++key) {
+                if ((key / kTileKeys - first) % STEP != 0) continue;
+                const int page = table[key >> a.page_log];
+                if (page < 0 || page >= a.pages) continue;
+                constexpr int ES = Tile32<DTYPE, D>::ES;
+                const uint8_t *row = a.V + (((((int64_t)page * a.h_kv + h) << a.page_log) + (key & ((1 << a.page_log) - 1))) * D) * ES;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        const int f = (4 * g + i) * NJ + j;
+                        const bool odd = DTYPE == PBS_BF16 ? (reinterpret_cast<const uint16_t *>(row)[f] & 0x7f80) == 0x7f80 : (row[f] & 0x7f) == 0x7f;
+                        const float v = DTYPE == PBS_BF16 ? (float)reinterpret_cast<const bf16_t *>(row)[f] : __uint_as_float(0x7fc00000u);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            if (odd && key < sees[nt]) st.o[j][nt][i] += v;
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        st.l[nt] += __shfl_xor(st.l[nt], 16, 64);
+        st.l[nt] += __shfl_xor(st.l[nt], 32, 64);
+    }
+}
+
+// A sum of zero, not a maximum of -inf, says that a query has met no key: NaN logits have no maximum.
+template <int N>
+__device__ __forceinline__ void store_output(const DecodeArgs &a, int token, int head, int f, const float (&o)[N], float m, float l)
+{
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    bf16_t *dst = a.O + (int64_t)token * a.o.token + (int64_t)head * a.o.head + f;
+#pragma unroll
+    for (int y = 0; y < N; y += 4) {
+        const floatx4 v = floatx4{o[y], o[y + 1], o[y + 2], o[y + 3]} * inv;
+        *reinterpret_cast<bf16x4 *>(dst + y) = __builtin_convertvector(v, bf16x4);
+    }
+    if (a.lse && f == 0) a.lse[(int64_t)token * a.h_q + head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+__device__ __forceinline__ int tiles_of(const DecodeArgs &a, int i) { return ceil_div(own_len(a, i), kTileKeys); }
+// what a unit of n tiles counts as: its start and its end cost a wave about as much as kUnitCost tiles
+__device__ __forceinline__ int cost_of(int n) { return n > 0 ? n + kUnitCost : 0; }
+
+// Sum over the workgroup, and in `before` the sum over the threads in front of this one.
+__device__ __forceinline__ int scan_group(int v, int &before, int *sums)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sum = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int other = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += other;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = sum;
+    __syncthreads();
+    int total = 0;
+    before = sum - v;
+#pragma unroll
+    for (int w = 0; w < kDecWaves; ++w) {
+        if (w < wave) before += sums[w];
+        total += sums[w];
+    }
+    return total;
+}
+
+// One piece of a unit (sequence i, unit k of it), tiles first .. last - 1, by one wave.  direct: it is the whole unit, and no prefix.
+template <int DTYPE, int D, int NT, bool SEVERAL>
+__device__ __forceinline__ void own_piece(const DecodeArgs &a, int i, int k, int len, int first, int last, int64_t slot, bool direct)
+{
+    constexpr int NJ = D / 16;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int tile = k / a.h_kv, h = k - tile * a.h_kv, rows = a.q_len * a.r, row0 = tile * 16 * NT;
+    DecodeState<D, NT> st;
+    walk_keys<DTYPE, D, NT, SEVERAL, true, 1>(st, a, a.table + (int64_t)i * a.max_pages, len, first, min(last * kTileKeys, len),
+                                              i * a.q_len, rows, row0, h);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int x = 16 * nt + c, row = row0 + x;
+        if (row >= rows) continue;
+        const int t = row / a.r, head = h * a.r + row - t * a.r;
+        const int64_t at = slot * a.slot_rows + x;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            float o[NJ];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[j] = st.o[j][nt][y];
+            const int f = (4 * g + y) * NJ;
+            if (direct) {
+                store_output(a, i * a.q_len + t, head, f, o, st.m[nt], st.l[nt]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NJ; j += 4)
+                    *reinterpret_cast<floatx4 *>(a.piece_o + at * D + f + j) = floatx4{o[j], o[j + 1], o[j + 2], o[j + 3]};
+            }
+        }
+        if (!direct && g == 0) {
+            a.piece_ml[2 * at] = st.m[nt];
+            a.piece_ml[2 * at + 1] = st.l[nt];
+        }
+    }
+}
+
+// WHOLE: a wave to a unit; otherwise an equal share of all tiles to a wave.
+template <int DTYPE, int D, int NT, bool SEVERAL, bool WHOLE>
+__global__ __launch_bounds__(kDecThreads, NT == 1 ? 2 : 1) void decode_own_kernel(DecodeArgs a)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int w = blockIdx.x * kDecWaves + wave;
+    if constexpr (WHOLE) {
+        const int i = w / a.units, len = i < a.n_seq ? own_len(a, i) : 0;
+        if (i < a.n_seq)
+            own_piece<DTYPE, D, NT, SEVERAL>(a, i, w - i * a.units, len, 0, ceil_div(len, kTileKeys), 0, true);
+        return;
+    }
+    __shared__ int sums[kDecWaves], found[kDecWaves];
+    __shared__ int64_t found_front[kDecWaves];
+    int64_t total = 0;
+    int before;
+    for (int base = 0; base < a.n_seq; base += kDecThreads) {
+        const int x = base + threadIdx.x;
+        total += scan_group(x < a.n_seq ? cost_of(tiles_of(a, x)) : 0, before, sums);
+    }
+    const int64_t share = max((total * a.units + a.shares - 1) / a.shares, (int64_t)1), all = total * a.units;
+    // the sequence that each wave's share begins in, and the cost of those in front of it
+    int64_t front = 0;
+    for (int base = 0; base < a.n_seq; base += kDecThreads) {
+        const int x = base + threadIdx.x, n = x < a.n_seq ? cost_of(tiles_of(a, x)) : 0;
+        const int sum = scan_group(n, before, sums);
+        const int64_t mine = (front + before) * a.units;
+#pragma unroll
+        for (int y = 0; y < kDecWaves; ++y) {
+            const int64_t at = (int64_t)(blockIdx.x * kDecWaves + y) * share;
+            if (mine <= at && at < mine + (int64_t)n * a.units) {
+                found[y] = x;
+                found_front[y] = mine;
+            }
+        }
+        front += sum;
+    }
+    __syncthreads();
+    int64_t at = w * share;
+    const int64_t stop = min(at + share, all);
+    if (at >= stop) return;
+    int i = __builtin_amdgcn_readfirstlane(found[wave]);
+    int len = __builtin_amdgcn_readfirstlane(own_len(a, i)), n = ceil_div(len, kTileKeys), cost = cost_of(n);
+    const int64_t inside = at - found_front[wave];         // of the sequence's units, in tiles
+    int k = __builtin_amdgcn_readfirstlane((int)(inside / cost)), off = __builtin_amdgcn_readfirstlane((int)(inside - (int64_t)k * cost));
+    while (true) {
+        const int take = (int)min((int64_t)(cost - off), stop - at);
+        const int first = max(off - kUnitCost, 0), last = off + take - kUnitCost;             // tiles
+        const int64_t unit = (int64_t)i * a.units + k, slot = w + unit;       // one of the two moves on with every piece
+        if (last > first) {
+            if (first == 0 && (threadIdx.x & 63) == 0)
+                a.pieces[unit] = make_int2(w, (int)((at - off + cost - 1) / share) - w + 1);
+            own_piece<DTYPE, D, NT, SEVERAL>(a, i, k, len, first, last, slot, first == 0 && last == n && a.p_parts == 0);
+        }
+        at += take;
+        if (at >= stop) break;
+        off = 0;
+        if (++k == a.units) {
+            k = 0;
+            do {
+                len = own_len(a, ++i);
+            } while (len == 0);                            // tiles are left, so there is a sequence with some
+            len = __builtin_amdgcn_readfirstlane(len);
+            n = ceil_div(len, kTileKeys);
+            cost = cost_of(n);
+        }
+    }
+}
+
 template <int DTYPE, int D, int NT>
-__device__ __forceinline__ void decode_part(const DecodeArgs &a, const int32_t *table, int len, int begin, int end, bool own,
-                                            int token0, int rows, int row0, int h, int part, bool single)
+__global__ __launch_bounds__(kDecThreads, NT == 1 ? 2 : 1) void decode_prefix_kernel(DecodeArgs a, bool single)
 {
     constexpr int NJ = D / 16;
     __shared__ __align__(16) float sum_o[kDecWaves][16][D + 4];
     __shared__ float sum_m[kDecWaves][NT * 16], sum_l[kDecWaves][NT * 16];
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    bf16x8 q[D / 32][NT];
-    int sees[NT];
+    const int h = blockIdx.x, row0 = blockIdx.y * 16 * NT, part = blockIdx.z;
+    const int begin = part * a.p_chunk, rows = a.n_seq * a.q_len * a.r;
     DecodeState<D, NT> st;
+    walk_keys<DTYPE, D, NT, false, false, kDecWaves>(st, a, a.prefix, a.prefix_len, begin / kTileKeys + wave,
+                                                     min(begin + a.p_chunk, a.prefix_len), 0, rows, row0, h);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int row = row0 + 16 * nt + c;
-        const bool there = row < rows;
-        const int rc = there ? row : rows - 1;
-        const int t = rc / a.r;
-        const bf16_t *src = a.Q + (int64_t)(token0 + t) * a.q.token + (int64_t)(h * a.r + rc - t * a.r) * a.q.head;
-#pragma unroll
-        for (int x = 0; x < D / 32; ++x)
-            q[x][nt] = *reinterpret_cast<const bf16x8 *>(src + (DTYPE == PBS_BF16 ? 32 * x + 8 * g : 64 * (x >> 1) + 16 * g + 8 * (x & 1)));
-        sees[nt] = own ? len - a.q_len + t + 1 : len;
-        st.m[nt] = -INFINITY;
-        st.l[nt] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) st.o[j][nt] = floatx4{0};
-    }
-    const int all = own ? len - a.q_len + 1 : len;
-
-    // this wave's tiles: wave, wave + 4, ...; lane x holds the page of 16 keys x of them
-    const int tiles = ceil_div(end - begin, kTileKeys);
-    const int mine = tiles > wave ? (tiles - wave + kDecWaves - 1) / kDecWaves : 0;
-    int held = -1;
-    {
-        const int key = begin + (wave + kDecWaves * (lane >> 1)) * kTileKeys + 16 * (lane & 1);
-        if ((lane >> 1) < mine && key < end) {
-            held = table[key >> a.page_log];
-            if (held >= a.pages) held = -1;
-        }
-    }
-    auto fetch = [&](Tile32<DTYPE, D> &t, int it) {
-        const int key0 = begin + (wave + kDecWaves * it) * kTileKeys;
-        const int page[2] = {__builtin_amdgcn_readlane(held, 2 * it), __builtin_amdgcn_readlane(held, 2 * it + 1)};
-        const int in_page = (1 << a.page_log) - 1;
-        const int place[2] = {key0 & in_page, (key0 + 16) & in_page};
-        load_tile<DTYPE, D>(t, a, page, place, h, c, g);
-    };
-    auto use = [&](const Tile32<DTYPE, D> &t, int it) {
-        multiply_tile<DTYPE, D, NT>(st, t, q, sees, begin + (wave + kDecWaves * it) * kTileKeys, all, len, a.c2, g);
-    };
-    Tile32<DTYPE, D> ta, tb;
-    if (mine > 0) fetch(ta, 0);
-    for (int it = 0; it < mine; it += 2) {
-        if (it + 1 < mine) fetch(tb, it + 1);
-        use(ta, it);
-        if (it + 1 < mine) {
-            if (it + 2 < mine) fetch(ta, it + 2);
-            use(tb, it + 1);
-        }
-    }
-
-    // join the four waves; a sum of zero, not a maximum of -inf, says that a query has met no key: NaN logits have no maximum
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        st.l[nt] += __shfl_xor(st.l[nt], 16, 64);
-        st.l[nt] += __shfl_xor(st.l[nt], 32, 64);
+    for (int nt = 0; nt < NT; ++nt)
         if (g == 0) {
             sum_m[wave][16 * nt + c] = st.m[nt];
             sum_l[wave][16 * nt + c] = st.l[nt];
         }
-    }
     __syncthreads();
-    const int64_t all_rows = (int64_t)a.n_seq * a.q_len * a.h_q;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         float m = -INFINITY;
@@ -381,21 +527,13 @@ __device__ __forceinline__ void decode_part(const DecodeArgs &a, const int32_t *
             }
             const int t = row / a.r, head = h * a.r + row - t * a.r;
             if (single) {
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                bf16_t *dst = a.O + (int64_t)(token0 + t) * a.o.token + (int64_t)head * a.o.head + f;
-#pragma unroll
-                for (int y = 0; y < NJ; y += 4) {
-                    const floatx4 v = floatx4{o[y], o[y + 1], o[y + 2], o[y + 3]} * inv;
-                    *reinterpret_cast<bf16x4 *>(dst + y) = __builtin_convertvector(v, bf16x4);
-                }
-                if (a.lse && (tid & 15) == 0)
-                    a.lse[(int64_t)(token0 + t) * a.h_q + head] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+                store_output(a, t, head, f, o, top, l);
             } else {
-                const int64_t at = part * all_rows + (int64_t)(token0 + t) * a.h_q + head;
+                const int64_t at = (int64_t)part * a.n_seq * a.q_len * a.h_q + (int64_t)t * a.h_q + head;
 #pragma unroll
                 for (int y = 0; y < NJ; y += 4)
                     *reinterpret_cast<floatx4 *>(a.part_o + at * D + f + y) = floatx4{o[y], o[y + 1], o[y + 2], o[y + 3]};
-                if ((tid & 15) == 0) {
+                if (f == 0) {
                     a.part_ml[2 * at] = top;
                     a.part_ml[2 * at + 1] = l;
                 }
@@ -405,75 +543,66 @@ __device__ __forceinline__ void decode_part(const DecodeArgs &a, const int32_t *
     }
 }
 
-// grid: x = kv head (consecutive workgroups, so that the XCDs share no page of a head), y = part * row tiles, z = sequence
-template <int DTYPE, int D, int NT>
-__global__ __launch_bounds__(kDecThreads, NT == 4 ? 1 : 2) void decode_own_kernel(DecodeArgs a, bool single)
-{
-    const int h = blockIdx.x, i = blockIdx.z;
-    const int part = blockIdx.y / a.row_tiles, tile = blockIdx.y - part * a.row_tiles;
-    const int len = own_len(a, i);
-    const int begin = part * a.chunk;
-    if (begin >= len && !single) return;                   // the joining launch knows which parts there are
-    decode_part<DTYPE, D, NT>(a, a.table + (int64_t)i * a.max_pages, len, min(begin, len), min(begin + a.chunk, len), true,
-                              i * a.q_len, a.q_len * a.r, tile * 16 * NT, h, a.p_parts + part, single);
-}
-
-template <int DTYPE, int D, int NT>
-__global__ __launch_bounds__(kDecThreads, NT == 4 ? 1 : 2) void decode_prefix_kernel(DecodeArgs a, bool single)
-{
-    const int h = blockIdx.x, tile = blockIdx.y, part = blockIdx.z;
-    const int begin = part * a.p_chunk;
-    decode_part<DTYPE, D, NT>(a, a.prefix, a.prefix_len, begin, min(begin + a.p_chunk, a.prefix_len), false, 0,
-                              a.n_seq * a.q_len * a.r, tile * 16 * NT, h, part, single);
-}
-
-// One workgroup of 4 x 32 threads (d = 64: 4 x 16) per row: every quarter takes every fourth part.
+// One workgroup per row, groups of D / 4 threads: every group takes every eighth (d = 64: sixteenth) of the prefix's parts and the
+// unit's pieces.  rows_of_unit: 16 NT.
 template <int D>
-__global__ __launch_bounds__(D) void decode_join_kernel(DecodeArgs a)
+__global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, int rows_of_unit)
 {
-    constexpr int L = D / 4;
-    __shared__ __align__(16) float so[4][D];
-    __shared__ float sm[4], sl[4];
+    constexpr int L = D / 4, G = kDecThreads / L;
+    __shared__ __align__(16) float so[G][D];
+    __shared__ float sl[G], sm[kDecWaves];
     const int64_t row = blockIdx.x, all_rows = (int64_t)a.n_seq * a.q_len * a.h_q;
     const int token = (int)(row / a.h_q), head = (int)(row - (int64_t)token * a.h_q);
-    const int quarter = threadIdx.x / L, x = threadIdx.x % L;
-    const int parts = a.p_parts + ceil_div(own_len(a, token / a.q_len), a.chunk);
-    float m = -INFINITY, l = 0.0f;
-    floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int p = quarter; p < parts; p += 4) {
-        const int64_t at = p * all_rows + row;
-        const float pm = a.part_ml[2 * at], pl = a.part_ml[2 * at + 1];
-        const floatx4 po = *reinterpret_cast<const floatx4 *>(a.part_o + at * D + 4 * x);
-        if (pl == 0.0f) continue;
-        const float top = fmaxf(m, pm);
-        const float was = __builtin_amdgcn_exp2f(m - top), now = __builtin_amdgcn_exp2f(pm - top);
-        o = o * was + po * now;
-        l = l * was + pl * now;
-        m = top;
-    }
-    *reinterpret_cast<floatx4 *>(&so[quarter][4 * x]) = o;
-    if (x == 0) { sm[quarter] = m; sl[quarter] = l; }
+    const int i = token / a.q_len, h = head / a.r, in_seq = (token - i * a.q_len) * a.r + head - h * a.r;
+    const int tile = in_seq / rows_of_unit;
+    const int64_t unit = (int64_t)i * a.units + tile * a.h_kv + h;
+    int2 own = make_int2(0, 0);
+    if (a.shares > 0 && own_len(a, i) > 0) own = a.pieces[unit];
+    if (a.p_parts == 0 && own.y == 1) return;              // stored where it was computed
+    const int64_t slot = own.x + unit;
+    const int all = a.p_parts + own.y;
+    auto place = [&](int p) {
+        return p < a.p_parts ? p * all_rows + row : (slot + p - a.p_parts) * a.slot_rows + in_seq - tile * rows_of_unit;
+    };
+    float m = -INFINITY;
+    for (int p = threadIdx.x; p < all; p += kDecThreads) m = fmaxf(m, (p < a.p_parts ? a.part_ml : a.piece_ml)[2 * place(p)]);
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
     __syncthreads();
-    if (quarter != 0) return;
-    const float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    const int group = threadIdx.x / L, x = threadIdx.x % L;
+    float l = 0.0f;
+    floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int p = group; p < all; p += G) {
+        const int64_t at = place(p);
+        const floatx2 ml = *reinterpret_cast<const floatx2 *>((p < a.p_parts ? a.part_ml : a.piece_ml) + 2 * at);
+        const floatx4 po = *reinterpret_cast<const floatx4 *>((p < a.p_parts ? a.part_o : a.piece_o) + at * D + 4 * x);
+        if (ml[1] != 0.0f) {                               // (NaN sums go through)
+            const float f = __builtin_amdgcn_exp2f(ml[0] - m);
+            l += ml[1] * f;
+            o += po * f;
+        }
+    }
+    *reinterpret_cast<floatx4 *>(&so[group][4 * x]) = o;
+    if (x == 0) sl[group] = l;
+    __syncthreads();
+    if (group != 0) return;
     l = 0.0f;
     o = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        if (sl[w] == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f(sm[w] - top);
-        l += sl[w] * f;
-        o += *reinterpret_cast<const floatx4 *>(&so[w][4 * x]) * f;
+    for (int w = 0; w < G; ++w) {
+        l += sl[w];
+        o += *reinterpret_cast<const floatx4 *>(&so[w][4 * x]);
     }
-    if (l != 0.0f) o *= 1.0f / l;
-    *reinterpret_cast<bf16x4 *>(a.O + (int64_t)token * a.o.token + (int64_t)head * a.o.head + 4 * x) = __builtin_convertvector(o, bf16x4);
-    if (a.lse && x == 0) a.lse[row] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    const float out[4] = {o[0], o[1], o[2], o[3]};
+    store_output(a, token, head, 4 * x, out, m, l);
 }
 
 // Tiles of 16 queries to a wave: enough for the rows where few.
 inline int tiles_for(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 
-// Keys of a part: the longest of 128, 256, ... 4096 with which the call has `wanted` workgroups.
+// Keys of a part of the prefix: the longest of 128, 256, ... 4096 with which the call has `wanted` workgroups.
 inline int part_keys(int64_t units, int64_t keys, int64_t wanted)
 {
     int chunk = kMostChunk;
@@ -484,8 +613,9 @@ inline int part_keys(int64_t units, int64_t keys, int64_t wanted)
 struct DecodePlan {
     DecodeArgs a;
     int nt, p_nt;
-    bool single;
-    size_t bytes, ml_at;
+    bool whole, join;
+    long long grid;                                        // workgroups of the own keys, 0: there are none
+    size_t bytes, part_o, part_ml, piece_o, piece_ml, pieces;   // of the workspace, and where in it
 };
 
 inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, DecodePlan &plan)
@@ -500,54 +630,71 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     if (p->dtype != PBS_BF16 || p->q_len > kMostQueries) return PBS_ERR_UNSUPPORTED;
     if ((long long)p->n_seq * p->q_len * p->h_q > 0x7fffffffLL || (long long)p->n_seq * p->max_pages > 0x7fffffffLL)
         return PBS_ERR_UNSUPPORTED;
-    if (p->n_seq > 65535) return PBS_ERR_UNSUPPORTED;
+    if (p->max_len > 1 << 27 || p->prefix_len > 1 << 27) return PBS_ERR_UNSUPPORTED;         // sums of tiles are ints
     DecodeArgs &a = plan.a;
     a.n_seq = p->n_seq; a.q_len = p->q_len; a.h_q = p->h_q; a.h_kv = c->h_kv; a.r = p->h_q / c->h_kv;
     a.page_log = log2_of(c->page); a.pages = c->pages; a.max_pages = p->max_pages;
-    a.max_len = (int)fmin((double)p->max_len, (double)p->max_pages * c->page);
+    const long long in_pages = (long long)p->max_pages * c->page;
+    a.max_len = p->max_len < in_pages ? p->max_len : (int)in_pages;
     a.prefix_len = p->prefix_len;
     a.c2 = (p->scale > 0.0f ? p->scale : (float)(1.0 / sqrt((double)c->d))) * 1.4426950408889634f;
     a.q = p->q; a.o = p->o;
     const int64_t rows = (int64_t)a.q_len * a.r, p_rows = rows * a.n_seq;
-    plan.nt = tiles_for(rows);
+    plan.nt = rows <= 16 ? 1 : 2;
     plan.p_nt = tiles_for(p_rows);
     a.row_tiles = (int)((rows + 16 * plan.nt - 1) / (16 * plan.nt));
+    a.units = a.h_kv * a.row_tiles;
+    a.slot_rows = (int)(rows < 16 * plan.nt ? rows : 16 * plan.nt);
     a.p_row_tiles = (int)((p_rows + 16 * plan.p_nt - 1) / (16 * plan.p_nt));
-    a.chunk = part_keys((int64_t)a.n_seq * a.h_kv * a.row_tiles, a.max_len, 1024);
-    const int64_t parts = ((int64_t)a.max_len + a.chunk - 1) / a.chunk;
-    a.p_chunk = part_keys((int64_t)a.h_kv * a.p_row_tiles, a.prefix_len, 1024);
+    a.p_chunk = part_keys((int64_t)a.h_kv * a.p_row_tiles, a.prefix_len, 128);
     const int64_t p_parts = ((int64_t)a.prefix_len + a.p_chunk - 1) / a.p_chunk;
-    if (parts * a.row_tiles > 65535 || p_parts > 65535 || a.p_row_tiles > 65535) return PBS_ERR_UNSUPPORTED;
-    a.parts = (int)parts;
+    if (p_parts > 65535 || a.p_row_tiles > 65535) return PBS_ERR_UNSUPPORTED;
     a.p_parts = (int)p_parts;
-    plan.single = a.parts + a.p_parts <= 1;
-    const size_t all = (size_t)a.n_seq * a.q_len * a.h_q * (size_t)(a.parts + a.p_parts);
-    plan.ml_at = align_up(all * c->d * 4, kWsAlign);
-    plan.bytes = plan.single ? 0 : plan.ml_at + align_up(all * 8, kWsAlign);
+    const long long units = (long long)a.n_seq * a.units, tiles = ((long long)a.max_len + kTileKeys - 1) / kTileKeys;
+    if (p->n_seq > 65535 || units > 0x7fffffffLL - 4096) return PBS_ERR_UNSUPPORTED;
+    plan.whole = a.p_parts == 0 && a.max_len <= kWholeKeys;
+    // what the chip holds at a time: two workgroups to a compute unit, one where they take all registers
+    const long long most = units * (tiles + kUnitCost);
+    a.shares = (plan.nt == 1 ? 512 : 256) * kDecWaves;
+    if (a.shares > most) a.shares = (int)most;
+    plan.grid = ((plan.whole ? units : a.max_len > 0 ? a.shares : 0) + kDecWaves - 1) / kDecWaves;
+    a.shares = (int)(plan.whole ? 0 : plan.grid * kDecWaves);
+    plan.join = !plan.whole && !(plan.grid == 0 && a.p_parts == 1);
+    const size_t all = plan.join ? (size_t)a.n_seq * a.q_len * a.h_q * (size_t)a.p_parts : 0;
+    const size_t slots = plan.join && plan.grid ? (size_t)(units + a.shares) * a.slot_rows : 0;
+    size_t at = 0;
+    auto room = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, kWsAlign); return here; };
+    plan.part_o = room(all * c->d * 4);
+    plan.piece_o = room(slots * c->d * 4);
+    plan.part_ml = room(all * 8);
+    plan.piece_ml = room(slots * 8);
+    plan.pieces = room(slots ? (size_t)units * 8 : 0);
+    plan.bytes = at;
     return PBS_OK;
+}
+
+template <int DTYPE, int D, bool SEVERAL, bool WHOLE>
+pbs_status launch_own(const DecodePlan &plan, hipStream_t s)
+{
+    auto kernel = plan.nt == 1 ? decode_own_kernel<DTYPE, D, 1, SEVERAL, WHOLE> : decode_own_kernel<DTYPE, D, 2, SEVERAL, WHOLE>;
+    return launch(kernel, dim3((unsigned)plan.grid), dim3(kDecThreads), 0, s, plan.a);
 }
 
 template <int DTYPE, int D>
 pbs_status launch_decode(const DecodePlan &plan, hipStream_t s)
 {
     const DecodeArgs &a = plan.a;
+    pbs_status st = PBS_OK;
     if (a.p_parts > 0) {
         auto kernel = plan.p_nt == 1 ? decode_prefix_kernel<DTYPE, D, 1>
                       : plan.p_nt == 2 ? decode_prefix_kernel<DTYPE, D, 2> : decode_prefix_kernel<DTYPE, D, 4>;
-        const pbs_status st = launch(kernel, dim3(a.h_kv, a.p_row_tiles, a.p_parts), dim3(kDecThreads), 0, s, a, plan.single);
-        if (st != PBS_OK) return st;
+        st = launch(kernel, dim3(a.h_kv, a.p_row_tiles, a.p_parts), dim3(kDecThreads), 0, s, a, !plan.join);
     }
-    if (a.parts > 0 || plan.single) {
-        if (!(plan.single && a.p_parts > 0)) {
-            auto kernel = plan.nt == 1 ? decode_own_kernel<DTYPE, D, 1>
-                          : plan.nt == 2 ? decode_own_kernel<DTYPE, D, 2> : decode_own_kernel<DTYPE, D, 4>;
-            const int parts = a.parts > 0 ? a.parts : 1;
-            const pbs_status st = launch(kernel, dim3(a.h_kv, parts * a.row_tiles, a.n_seq), dim3(kDecThreads), 0, s, a, plan.single);
-            if (st != PBS_OK) return st;
-        }
-    }
-    if (plan.single) return PBS_OK;
-    return launch(decode_join_kernel<D>, dim3((unsigned)((int64_t)a.n_seq * a.q_len * a.h_q)), dim3(D), 0, s, a);
+    if (st == PBS_OK && plan.grid > 0)
+        st = a.q_len == 1 ? (plan.whole ? launch_own<DTYPE, D, false, true>(plan, s) : launch_own<DTYPE, D, false, false>(plan, s))
+                          : (plan.whole ? launch_own<DTYPE, D, true, true>(plan, s) : launch_own<DTYPE, D, true, false>(plan, s));
+    if (st != PBS_OK || !plan.join) return st;
+    return launch(decode_join_kernel<D>, dim3((unsigned)((int64_t)a.n_seq * a.q_len * a.h_q)), dim3(kDecThreads), 0, s, a, 16 * plan.nt);
 }
 
 }  // namespace pbs
@@ -587,8 +734,12 @@ extern "C" pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cac
     a.prefix = prefix_pages;
     a.O = static_cast<bf16_t *>(O);
     a.lse = lse;
-    a.part_o = static_cast<float *>(ws);
-    a.part_ml = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + plan.ml_at);
+    uint8_t *room = static_cast<uint8_t *>(ws);
+    a.part_o = reinterpret_cast<float *>(room + plan.part_o);
+    a.part_ml = reinterpret_cast<float *>(room + plan.part_ml);
+    a.piece_o = reinterpret_cast<float *>(room + plan.piece_o);
+    a.piece_ml = reinterpret_cast<float *>(room + plan.piece_ml);
+    a.pieces = reinterpret_cast<int2 *>(room + plan.pieces);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (c->d == 128)
         return c->dtype == PBS_BF16 ? launch_decode<PBS_BF16, 128>(plan, s)
