@@ -17,8 +17,7 @@
 // cut into parts of its keys, and its rows are the queries of the whole batch: its keys are read once.
 #include <type_traits>
 
-#include "pbs_host.h"
-#include "serving.h"
+#include "decode.h"
 
 namespace pbs {
 
@@ -30,25 +29,6 @@ constexpr int kHeldTiles = 32;                             // tiles whose pages 
 constexpr int kWholeKeys = 128;                            // lengths up to which a unit has a wave to itself
 constexpr int kUnitCost = 2;                               // tiles
 constexpr int kMostQueries = 16;
-
-struct DecodeArgs {
-    int n_seq, q_len, h_q, h_kv, r;
-    int page_log, pages, max_pages, max_len, prefix_len;
-    int row_tiles;                                         // of a sequence's q_len * r rows
-    int units;                                             // of a sequence: h_kv * row_tiles
-    int shares;                                            // waves of the own keys
-    int slot_rows;                                         // rows of a piece in the workspace
-    int p_chunk, p_parts, p_row_tiles;                     // the same of the prefix
-    float c2;                                              // scale * log2(e)
-    pbs_strides q, o;
-    const bf16_t *Q;
-    const uint8_t *K, *V;
-    const float *kf, *vf;
-    const int32_t *table, *lens, *prefix;
-    bf16_t *O;
-    float *lse, *part_o, *part_ml, *piece_o, *piece_ml;
-    int2 *pieces;                                          // of a unit: its first slot and how many
-};
 
 // own keys of sequence i
 __device__ __forceinline__ int own_len(const DecodeArgs &a, int i)
@@ -79,22 +59,6 @@ struct Tile32<PBS_E4M3, 64> {
 };
 template <>
 struct Tile32<PBS_I8, 64> : Tile32<PBS_E4M3, 64> {};
-
-// four 8-bit values as two pairs of bf16
-template <int DTYPE>
-__device__ __forceinline__ uintx2 widen4(uint32_t w)
-{
-    if constexpr (DTYPE == PBS_E4M3) {
-        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
-        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
-        return uintx2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-    } else {
-        const floatx2 a = {(float)(int)(int8_t)w, (float)(int)(int8_t)(w >> 8)};
-        const floatx2 b = {(float)(int)(int8_t)(w >> 16), (float)(int)(int8_t)(w >> 24)};
-        return uintx2{__builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)),
-                      __builtin_bit_cast(uint32_t, __builtin_convertvector(b, bf16x2))};
-    }
-}
 
 // The 16 rows of sub-tile u start at row `first` of the cache's rows (a head's rows of a page are consecutive).
 template <int DTYPE, int D>
@@ -599,9 +563,6 @@ __global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, 
     store_output(a, token, head, 4 * x, out, m, l);
 }
 
-// Tiles of 16 queries to a wave: enough for the rows where few.
-inline int tiles_for(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
-
 // Keys of a part of the prefix: the longest of 128, 256, ... 4096 with which the call has `wanted` workgroups.
 inline int part_keys(int64_t units, int64_t keys, int64_t wanted)
 {
@@ -615,7 +576,8 @@ struct DecodePlan {
     int nt, p_nt;
     bool whole, join;
     long long grid;                                        // workgroups of the own keys, 0: there are none
-    size_t bytes, part_o, part_ml, piece_o, piece_ml, pieces;   // of the workspace, and where in it
+    size_t bytes;                                          // of the workspace, and where in it:
+    size_t part_o, part_ml, piece_o, piece_ml, pieces, line_k, line_v, line_kf, line_vf;
 };
 
 inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, DecodePlan &plan)
@@ -641,12 +603,21 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     a.q = p->q; a.o = p->o;
     const int64_t rows = (int64_t)a.q_len * a.r, p_rows = rows * a.n_seq;
     plan.nt = rows <= 16 ? 1 : 2;
-    plan.p_nt = tiles_for(p_rows);
+    plan.p_nt = p_rows <= 16 ? 1 : p_rows <= 32 ? 2 : 0;   // 0: the kernel for many rows
     a.row_tiles = (int)((rows + 16 * plan.nt - 1) / (16 * plan.nt));
     a.units = a.h_kv * a.row_tiles;
     a.slot_rows = (int)(rows < 16 * plan.nt ? rows : 16 * plan.nt);
-    a.p_row_tiles = (int)((p_rows + 16 * plan.p_nt - 1) / (16 * plan.p_nt));
-    a.p_chunk = part_keys((int64_t)a.h_kv * a.p_row_tiles, a.prefix_len, 128);
+    const int64_t p_tile = plan.p_nt ? 16 * plan.p_nt : kPrefixRows;
+    a.p_row_tiles = (int)((p_rows + p_tile - 1) / p_tile);
+    if (plan.p_nt) {
+        a.p_chunk = part_keys((int64_t)a.h_kv * a.p_row_tiles, a.prefix_len, 128);
+    } else {
+        // two workgroups to a compute unit, whole turns of the loop, pages of a part in a wave's lanes
+        const int64_t units = (int64_t)a.h_kv * a.p_row_tiles, parts = (512 + units - 1) / units;
+        a.p_chunk = (int)(((a.prefix_len + parts - 1) / parts + 127) / 128 * 128);
+        if (a.p_chunk > 1024) a.p_chunk = 1024;
+        if (a.p_chunk < 128) a.p_chunk = 128;
+    }
     const int64_t p_parts = ((int64_t)a.prefix_len + a.p_chunk - 1) / a.p_chunk;
     if (p_parts > 65535 || a.p_row_tiles > 65535) return PBS_ERR_UNSUPPORTED;
     a.p_parts = (int)p_parts;
@@ -669,6 +640,13 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     plan.part_ml = room(all * 8);
     plan.piece_ml = room(slots * 8);
     plan.pieces = room(slots ? (size_t)units * 8 : 0);
+    const bool line = a.p_parts > 0 && plan.p_nt == 0 && c->dtype != PBS_BF16;
+    a.p_room = line ? (a.prefix_len + 127) / 128 * 128 : 0;
+    const size_t line_rows = (size_t)a.h_kv * a.p_room;
+    plan.line_k = room(line_rows * c->d * 2);
+    plan.line_v = room(line_rows * c->d * 2);
+    plan.line_kf = room(line_rows * 4);
+    plan.line_vf = room(line_rows * 4);
     plan.bytes = at;
     return PBS_OK;
 }
@@ -685,9 +663,10 @@ pbs_status launch_decode(const DecodePlan &plan, hipStream_t s)
 {
     const DecodeArgs &a = plan.a;
     pbs_status st = PBS_OK;
-    if (a.p_parts > 0) {
-        auto kernel = plan.p_nt == 1 ? decode_prefix_kernel<DTYPE, D, 1>
-                      : plan.p_nt == 2 ? decode_prefix_kernel<DTYPE, D, 2> : decode_prefix_kernel<DTYPE, D, 4>;
+    if (a.p_parts > 0 && plan.p_nt == 0) {
+        st = launch_prefix(a, DTYPE, D, !plan.join, s);
+    } else if (a.p_parts > 0) {
+        auto kernel = plan.p_nt == 1 ? decode_prefix_kernel<DTYPE, D, 1> : decode_prefix_kernel<DTYPE, D, 2>;
         st = launch(kernel, dim3(a.h_kv, a.p_row_tiles, a.p_parts), dim3(kDecThreads), 0, s, a, !plan.join);
     }
     if (st == PBS_OK && plan.grid > 0)
@@ -740,6 +719,10 @@ extern "C" pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cac
     a.piece_o = reinterpret_cast<float *>(room + plan.piece_o);
     a.piece_ml = reinterpret_cast<float *>(room + plan.piece_ml);
     a.pieces = reinterpret_cast<int2 *>(room + plan.pieces);
+    a.line_k = reinterpret_cast<bf16_t *>(room + plan.line_k);
+    a.line_v = reinterpret_cast<bf16_t *>(room + plan.line_v);
+    a.line_kf = reinterpret_cast<float *>(room + plan.line_kf);
+    a.line_vf = reinterpret_cast<float *>(room + plan.line_vf);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (c->d == 128)
         return c->dtype == PBS_BF16 ? launch_decode<PBS_BF16, 128>(plan, s)

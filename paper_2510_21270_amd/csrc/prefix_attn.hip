@@ -1,0 +1,177 @@
+// The prefix of pbs_decode_attn against many rows: the queries of the whole batch, 128 to a workgroup, on the pipeline of
+// key_pipeline.h.  A part of the keys and a kv head to a workgroup; O, m and l of every part go to the workspace.
+//
+// A bf16 cache is read where its pages lie.  8-bit values are first written out as bf16, in order, the factors beside them: the
+// pipeline has no room for the widening of every tile in every workgroup, and the prefix is short beside what is done with it.
+#include "decode.h"
+#include "key_pipeline.h"
+
+namespace pbs {
+namespace prompt {
+
+// Tiles of a part from the pages of a cache.  held: the pages of the part's 32 tiles in a wave's lanes, two to a tile.  The halves of a
+// tile have a descriptor each, which ends with the keys that exist: what lies behind them reads as zeros.
+template <int D>
+struct Pages {
+    const bf16_t *pool;
+    int held, count, begin, page_log, h, h_kv;
+    struct At {
+        __amdgpu_buffer_rsrc_t lo, hi;
+        __device__ __forceinline__ void pin() {}
+    };
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t half(int t, int u) const
+    {
+        const int page = __builtin_amdgcn_readlane(held, (2 * t + u) & 63), rows = min(count - t * KS, KS);
+        const int place = (begin + t * KS + 16 * u) & ((1 << page_log) - 1);
+        const bf16_t *base = pool + (((((int64_t)max(page, 0)) * h_kv + h) << page_log) + place - 16 * u) * D;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(base), 0, page >= 0 && rows > 16 * u ? rows * D * 2 : 0, 0x00020000);
+    }
+    __device__ __forceinline__ At at(int t) const { return {half(t, 0), half(t, 1)}; }
+    __device__ __forceinline__ void load(unsigned char *dst, int c, const At &w, const Offsets<D> &off) const
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(c < Offsets<D>::kLoads / 2 ? w.lo : w.hi, (lptr_t)(dst + c * 1024), 16, off.from[c], 0, 0, 0);
+    }
+    __device__ __forceinline__ void load_factors(float *, int, int) const {}
+};
+
+// LINE: the keys lie in order as bf16 with factors beside them.
+template <int D, bool LINE>
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void prefix_kernel(DecodeArgs a, bool single)
+{
+    __shared__ Stage<D, LINE> sg0, sg1, sg2, sg3;
+    __shared__ int bad_rows;
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kv = blockIdx.x, row0 = blockIdx.y * kPrefixRows, part = blockIdx.z;
+    const int begin = part * a.p_chunk, count = min(a.p_chunk, a.prefix_len - begin), tiles = (count + KS - 1) / KS;
+    const int rows = a.n_seq * a.q_len * a.r;
+
+    int held = -1;
+    bool bad = false;
+    if (lane < (count + 15) / 16) {
+        held = a.prefix[(begin + 16 * lane) >> a.page_log];
+        if (held >= a.pages) held = -1;
+        bad = held < 0;
+    }
+    bf16x8 q[2][D / 16];
+    const int sees[2] = {count, count};
+    auto load_queries = [&]() {
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const int row = min(row0 + wave * 64 + 32 * nt + n, rows - 1), t = row / a.r;
+            const bf16_t *src = a.Q + (int64_t)t * a.q.token + (int64_t)(kv * a.r + row - t * a.r) * a.q.head + 8 * h;
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) q[nt][x] = *reinterpret_cast<const bf16x8 *>(src + 16 * x);
+        }
+    };
+    auto source = [&]() {
+        if constexpr (LINE) {
+            Rows<D, true> s;
+            const int64_t first = (int64_t)kv * a.p_room + begin;
+            s.size = count * D * 2;
+            s.tile_bytes = KS * D * 2;
+            s.factors_size = min(a.p_chunk, a.p_room - begin) * 4;
+            s.rows = __builtin_amdgcn_make_buffer_rsrc((wave == 0 ? a.line_k : a.line_v) + first * D, 0, s.size, 0x00020000);
+            s.factors = __builtin_amdgcn_make_buffer_rsrc((wave == 0 ? a.line_kf : a.line_vf) + first, 0, s.factors_size, 0x00020000);
+            return s;
+        } else {
+            return Pages<D>{reinterpret_cast<const bf16_t *>(wave == 0 ? a.K : a.V), held, count, begin, a.page_log, kv, a.h_kv};
+        }
+    };
+    auto store = [&](const State<D> &st) {
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const int row = row0 + wave * 64 + 32 * nt + n;
+            const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64);
+            if (row >= rows) continue;
+            const int t = row / a.r, head = kv * a.r + row - t * a.r;
+            const int64_t out = (int64_t)t * a.h_q + head, at = (int64_t)part * a.n_seq * a.q_len * a.h_q + out;
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const floatx16 &o = st.o[dt][nt];
+                    const floatx4 v = {o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]};
+                    const int f = 32 * dt + 8 * x + 4 * h;
+                    if (single)
+                        *reinterpret_cast<bf16x4 *>(a.O + (int64_t)t * a.o.token + (int64_t)head * a.o.head + f) =
+                            __builtin_convertvector(l == 0.0f ? floatx4{0} : v * inv, bf16x4);
+                    else
+                        *reinterpret_cast<floatx4 *>(a.part_o + at * D + f) = v;
+                }
+            if (h == 0 && !single) {
+                a.part_ml[2 * at] = st.m[nt];
+                a.part_ml[2 * at + 1] = l;
+            } else if (h == 0 && a.lse) {
+                a.lse[out] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            }
+        }
+    };
+    load_queries();
+    const auto src = source();
+    const Offsets<D> off = offsets<D>(wave, lane, D * 2);
+    const unsigned long long missing = __ballot(bad);      // sixteens of keys in no page
+    if (threadIdx.x == 0) bad_rows = 0;
+    {
+        State<D> st;
+        clear(st);
+        bad = all_tiles<D, LINE>(st, q, sees, count, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane) || missing != 0;
+        store(st);
+    }
+    meet();
+    if (__any(bad) && lane == 0) bad_rows = 1;
+    __syncthreads();
+    if (__builtin_expect(bad_rows != 0, 0)) {
+        State<D> st;
+        clear(st);
+        load_queries();
+        for (int t = 0; t < tiles; ++t) {
+            __syncthreads();
+            issue_tile(sg0, src, off, t, wave);
+            issue_factors(sg0, src, t, wave, lane);
+            meet();
+            whole_tile<D, LINE>(st, sg0, off, q, sees, t * KS, (int)(~missing >> (2 * t)) & 3, a.c2, h);
+        }
+        store(st);
+    }
+}
+
+// The prefix's 8-bit values as bf16, eight to a thread, and their factors; rows behind the prefix and in no page: zeros, 1.
+template <int DTYPE, int D>
+__global__ __launch_bounds__(256) void line_kernel(DecodeArgs a)
+{
+    constexpr int L = D / 8;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int row = (int)(at / L), x = (int)at % L, h = blockIdx.y;
+    if (row >= a.p_room) return;
+    int page = -1;
+    if (row < a.prefix_len) page = a.prefix[row >> a.page_log];
+    const bool there = page >= 0 && page < a.pages;
+    const int64_t from = (((int64_t)(there ? page : 0) * a.h_kv + h) << a.page_log) + (row & ((1 << a.page_log) - 1));
+    const int64_t to = (int64_t)h * a.p_room + row;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        uint2 w = make_uint2(0, 0);
+        if (there) w = *reinterpret_cast<const uint2 *>((v ? a.V : a.K) + from * D + 8 * x);
+        const uintx2 lo = widen4<DTYPE>(w.x), hi = widen4<DTYPE>(w.y);
+        *reinterpret_cast<uintx4 *>((v ? a.line_v : a.line_k) + to * D + 8 * x) = uintx4{lo[0], lo[1], hi[0], hi[1]};
+        if (x == 0) (v ? a.line_vf : a.line_kf)[to] = there ? (v ? a.vf : a.kf)[from] : 1.0f;
+    }
+}
+
+}  // namespace prompt
+
+pbs_status launch_prefix(const DecodeArgs &a, int dtype, int d, bool single, hipStream_t s)
+{
+    using namespace prompt;
+    const dim3 grid(a.h_kv, a.p_row_tiles, a.p_parts), block(128);
+    if (dtype == PBS_BF16) return launch(d == 128 ? prefix_kernel<128, false> : prefix_kernel<64, false>, grid, block, 0, s, a, single);
+    auto line = d == 128 ? (dtype == PBS_E4M3 ? line_kernel<PBS_E4M3, 128> : line_kernel<PBS_I8, 128>)
+                         : (dtype == PBS_E4M3 ? line_kernel<PBS_E4M3, 64> : line_kernel<PBS_I8, 64>);
+    const pbs_status st = launch(line, dim3((unsigned)(((int64_t)a.p_room * (d / 8) + 255) / 256), a.h_kv), dim3(256), 0, s, a);
+    if (st != PBS_OK) return st;
+    return launch(d == 128 ? prefix_kernel<128, true> : prefix_kernel<64, true>, grid, block, 0, s, a, single);
+}
+
+}  // namespace pbs

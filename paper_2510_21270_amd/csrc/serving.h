@@ -43,6 +43,22 @@ inline int log2_of(int v)
     return l;
 }
 
+// four 8-bit values as two pairs of bf16
+template <int DTYPE>
+__device__ __forceinline__ uintx2 widen4(uint32_t w)
+{
+    if constexpr (DTYPE == PBS_E4M3) {
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
+        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+        return uintx2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+    } else {
+        const floatx2 a = {(float)(int)(int8_t)w, (float)(int)(int8_t)(w >> 8)};
+        const floatx2 b = {(float)(int)(int8_t)(w >> 16), (float)(int)(int8_t)(w >> 24)};
+        return uintx2{__builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)),
+                      __builtin_bit_cast(uint32_t, __builtin_convertvector(b, bf16x2))};
+    }
+}
+
 // eight consecutive elements as float, and back with one rounding
 __device__ __forceinline__ void load8(const bf16_t *p, float (&x)[8])
 {

@@ -273,6 +273,52 @@ def test_decode_shared_prefix(n_seq, q_len, h_q, h_kv, d, prefix, held):
     s.check(O, lse)
 
 
+@pytest.mark.parametrize("held", ["bf16", "e4m3", "i8"])
+@pytest.mark.parametrize("h_q,h_kv,d,page,prefix", [(8, 2, 128, 16, 1), (8, 1, 128, 64, 127), (8, 2, 64, 32, 128), (16, 4, 64, 16, 129), (12, 1, 128, 128, 1500),
+                                                    (7, 1, 64, 256, 3333)])
+def test_decode_prefix_of_a_large_batch(h_q, h_kv, d, page, prefix, held):
+    # more rows than a wave takes: several workgroups of 128, the last one partly filled
+    n = 13 if prefix < 1000 else 21
+    s = Setup(30, 1, h_q, h_kv, d, held, page, [(5 * i) % 40 for i in range(n)], prefix)
+    O, lse = s.call(want_lse=True)
+    s.check(O, lse)
+    again = s.call()
+    assert torch.equal(O, again)
+
+
+@pytest.mark.parametrize("held", ["bf16", "e4m3"])
+def test_decode_prefix_of_a_large_batch_with_odd_pages_and_values(held):
+    s = Setup(31, 1, 16, 2, 128, held, 16, [3] * 9, 300)
+    s.prefix_pages[4], s.prefix_pages[11] = -1, 77777
+
+    def hidden(i, j):
+        return ((j >= 64) & (j < 80)) | ((j >= 176) & (j < 192))
+
+    O, lse = s.call(want_lse=True)
+    s.check(O, lse, hidden)
+    # a value that is not finite in a key that everybody sees
+    page = int(s.prefix_pages[2])
+    if held == "bf16":
+        s.cache.V[page, 1, 3, 9] = math.inf
+    else:
+        s.cache.v_scale[page, 1, 3] = math.nan
+    got = s.call().float().cpu()
+    assert torch.isfinite(got[:, :, :8]).all()
+    if held == "bf16":
+        assert (got[:, :, 8:, 9] == math.inf).all()
+        got[:, :, 8:, 9] = 0
+        assert torch.isfinite(got).all()
+    else:
+        assert torch.isnan(got[:, :, 8:]).all()
+
+
+def test_decode_prefix_of_a_large_batch_logits_that_grow():
+    s = Setup(32, 1, 40, 1, 128, "i8", 32, [5], 900)
+    s.Q *= 30                                              # hundreds of nats between keys
+    O, lse = s.call(want_lse=True)
+    s.check(O, lse)
+
+
 def test_decode_prefix_alone_and_nothing_at_all():
     s = Setup(4, 1, 8, 2, 128, "bf16", 16, [0, 0, 0], 50)
     O, lse = s.call(want_lse=True)
