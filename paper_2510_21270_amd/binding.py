@@ -6,6 +6,7 @@ or a call fails, an exception is raised.
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -98,15 +99,16 @@ def load_library():
         lib.pbs_mass_covered.argtypes = [P, V, V, V, V]
         lib.pbs_mfma_rate_probe.argtypes = [ctypes.c_int, ctypes.c_int, V, Z, ctypes.POINTER(ctypes.c_double), V]
         lib.pbs_shader_clock_meter.argtypes = [V, ctypes.c_int, V]
-        D, I, S, C = ctypes.c_double, ctypes.c_int32, ctypes.POINTER(pbs_strides), ctypes.POINTER(pbs_cache)
-        lib.pbs_rope.argtypes = [ctypes.POINTER(pbs_rope_problem), V, V, V, V, V, V, V]
+        # (structures of the calls below are passed as addresses: ctypes objects by byref, packed bytes as they are)
+        D, I = ctypes.c_double, ctypes.c_int32
+        lib.pbs_rope.argtypes = [V, V, V, V, V, V, V, V]
         lib.pbs_rope_frequencies.argtypes = [ctypes.c_int, I, D, D, D, D, D, ctypes.POINTER(D), ctypes.POINTER(D)]
-        lib.pbs_cache_write.argtypes = [C, I, I, V, S, V, S, V, V]
-        lib.pbs_cache_read.argtypes = [C, I, I, V, V, S, V, S, V]
+        lib.pbs_cache_write.argtypes = [V, I, I, V, V, V, V, V, V]
+        lib.pbs_cache_read.argtypes = [V, I, I, V, V, V, V, V, V]
         lib.pbs_decode_workspace_bytes.restype = Z
-        lib.pbs_decode_workspace_bytes.argtypes = [ctypes.POINTER(pbs_decode_problem), C]
-        lib.pbs_decode_attn.argtypes = [ctypes.POINTER(pbs_decode_problem), C, V, V, V, V, V, V, V, Z, V]
-        lib.pbs_prompt_attn.argtypes = [ctypes.POINTER(pbs_prompt_problem), V, V, V, V, V, V, V, V]
+        lib.pbs_decode_workspace_bytes.argtypes = [V, V]
+        lib.pbs_decode_attn.argtypes = [V, V, V, V, V, V, V, V, V, Z, V]
+        lib.pbs_prompt_attn.argtypes = [V, V, V, V, V, V, V, V, V]
         _lib = lib
     return _lib
 
@@ -352,53 +354,53 @@ def shader_clock_beside(fn, micros=20000, delay_s=0.02):
 
 # ---------------------------------------------------------------------------------------------------------------
 # Around the prefill path: tensors of [tokens, heads, d] with any token and head strides (a slice of a fused projection, a
-# transposed [heads, n, d] tensor).  The checks here are those that the library cannot make: sizes, types and devices of tensors.
+# transposed [heads, n, d] tensor).  The checks here are those that the library cannot make: sizes, types and devices of
+# tensors.  A step of single tokens is a handful of these calls, so they are kept short: arguments are packed into the
+# library's structures in one go (the layouts of pbs_rope_problem, ... above).
+_DTYPE_CODES = {torch.float32: PBS_F32, torch.bfloat16: PBS_BF16, torch.float8_e4m3fn: PBS_E4M3, torch.int8: PBS_I8}
+_STRIDES = struct.Struct("2q").pack
+_ROPE = struct.Struct("7ifI8q").pack
+_CACHE = struct.Struct("5i4P").pack
+_DECODE = struct.Struct("7if4q").pack
+_PROMPT = struct.Struct("7ifI8q").pack
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
-def _need(ok, what, why):
-    if not ok:
-        raise PbsError("%s: %s" % (what, why))
+
+def _refuse(what, why):
+    raise PbsError("%s: %s" % (what, why))
 
 
-def _device_of(what, *tensors):
-    """The device of all tensors given; they have to agree and to be on a GPU."""
-    dev = None
+def _same_device(what, dev, *tensors):
+    """All tensors (None: not given) lie on GPU `dev`."""
+    if dev < 0:
+        _refuse(what, "a tensor is not on the GPU")
     for t in tensors:
-        if t is not None:
-            _need(t.is_cuda, what, "a tensor is not on the GPU")
-            _need(dev is None or t.device == dev, what, "tensors on different devices")
-            dev = t.device
-    return dev
+        if t is not None and t.get_device() != dev:
+            _refuse(what, "tensors on different devices")
 
 
 def _launch(what, dev, fn, *args):
-    """fn(*args, stream) on the current stream of `dev`, whatever device is current."""
-    if dev.index == torch.cuda.current_device():
-        st = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    """fn(*args, stream) on the current stream of GPU `dev`, whatever device is current."""
+    if dev == torch._C._cuda_getDevice():
+        st = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            st = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
-    _check(st, what)
+            st = fn(*args, _raw_stream(dev))
+    if st != 0:
+        _check(st, what)
 
 
-def _addr(t):
-    return None if t is None else t.data_ptr()
-
-
-_DTYPE_CODES = {torch.float32: PBS_F32, torch.bfloat16: PBS_BF16, torch.float8_e4m3fn: PBS_E4M3, torch.int8: PBS_I8}
-_NO_STRIDES = pbs_strides(0, 0)
-
-
-def _rows(what, x, name, d=None):
-    """Strides of a [tokens, heads, d] tensor whose features are consecutive."""
-    _need(x.dim() == 3 and (d is None or x.shape[2] == d), what, "%s has to be [tokens, heads, d]" % name)
-    st, sh, sd = x.stride()
-    _need(sd == 1 or x.numel() == 0, what, "the features of %s are not consecutive" % name)
-    return pbs_strides(st if x.shape[0] > 1 else 0, sh if x.shape[1] > 1 else 0)
+def _rows(what, x):
+    """(token, head) strides of a [tokens, heads, d] tensor whose features are consecutive."""
+    (n, h, _), (st, sh, sd) = x.shape, x.stride()
+    if sd != 1 and x.numel():
+        _refuse(what, "the features of a tensor are not consecutive")
+    return (st if n > 1 else 0, sh if h > 1 else 0)
 
 
 def _ints(what, x, name, *shape):
-    _need(x.dtype == torch.int32 and x.is_contiguous() and tuple(x.shape) == shape, what,
-          "%s has to be contiguous int32 of shape %s" % (name, list(shape)))
+    if x.dtype != torch.int32 or x.shape != shape or not x.is_contiguous():
+        _refuse(what, "%s has to be contiguous int32 of shape %s" % (name, list(shape)))
 
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -409,7 +411,8 @@ ROPE_TRANSPOSE = 1
 def rope_frequencies(rot, base=1e4, scaling=None, factor=1.0, original=4096, low=None, high=None, device="cuda"):
     """(frequencies [rot / 2] float64 on `device`, magnitude) of rotary pairs, scaled for contexts longer than `original`:
     None, "linear", "bands" (low, high: turns over the original context, 1 and 4) or "ramp" (1 and 32)."""
-    _need(scaling in ROPE_SCALINGS, "pbs_rope_frequencies", "unknown scaling %r" % (scaling,))
+    if scaling not in ROPE_SCALINGS:
+        _refuse("pbs_rope_frequencies", "unknown scaling %r" % (scaling,))
     low = 1.0 if low is None else low
     high = (32.0 if scaling == "ramp" else 4.0) if high is None else high
     table, mag = (ctypes.c_double * max(1, rot // 2))(), ctypes.c_double(0.0)
@@ -421,32 +424,43 @@ def rope_frequencies(rot, base=1e4, scaling=None, factor=1.0, original=4096, low
 def rope(Q, K, positions, freq, layout="half", magnitude=1.0, transpose=False, Qout=None, Kout=None):
     """Q and K (either may be None) turned by their positions; new tensors, or in place with Qout=Q, Kout=K."""
     what = "pbs_rope"
-    dev = _device_of(what, Q, K, positions, freq, Qout, Kout)
-    one = Q if Q is not None else K
-    _need(one is not None, what, "neither Q nor K")
-    _need(layout in ROPE_LAYOUTS, what, "unknown layout %r" % (layout,))
-    _need(magnitude != 0.0, what, "magnitude 0")
-    tokens, d = one.shape[0], one.shape[-1]
-    _ints(what, positions, "positions", tokens)
-    _need(freq.dtype == torch.float64 and freq.dim() == 1 and freq.is_contiguous(), what, "freq has to be contiguous float64")
+    x = Q if Q is not None else K
+    if x is None:
+        _refuse(what, "neither Q nor K")
+    dev, dt = x.get_device(), x.dtype
+    if dev < 0:
+        _refuse(what, "a tensor is not on the GPU")
     if Q is not None and Qout is None:
-        Qout = torch.empty(Q.shape, dtype=Q.dtype, device=dev)
+        Qout = torch.empty_like(Q)
     if K is not None and Kout is None:
-        Kout = torch.empty(K.shape, dtype=K.dtype, device=dev)
-    p = pbs_rope_problem(tokens, 0, 0, d, 2 * freq.shape[0], ROPE_LAYOUTS[layout], _DTYPE_CODES.get(one.dtype, -1),
-                         magnitude, ROPE_TRANSPOSE if transpose else 0)
-    for x, out, name in ((Q, Qout, "Q"), (K, Kout, "K")):
-        _need((x is None) == (out is None), what, "%sout without %s" % (name, name))
-        if x is None:
+        Kout = torch.empty_like(K)
+    _same_device(what, dev, Q, K, Qout, Kout, positions, freq)
+    if x.dim() != 3:
+        _refuse(what, "Q and K have to be [tokens, heads, d]")
+    tokens, _, d = x.shape
+    _ints(what, positions, "positions", tokens)
+    if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous():
+        _refuse(what, "freq has to be contiguous float64 [rot / 2]")
+    if layout not in ROPE_LAYOUTS or magnitude == 0.0:
+        _refuse(what, "unknown layout %r or magnitude 0" % (layout,))
+    heads, strides, places = [0, 0], (), []
+    for k, (t, out) in enumerate(((Q, Qout), (K, Kout))):
+        if t is None:
+            if out is not None:
+                _refuse(what, "an output without its input")
+            strides += (0, 0, 0, 0)
+            places.append((None, None))
             continue
-        _need(x.shape[0] == tokens and x.dtype == one.dtype and out.dtype == x.dtype and out.shape == x.shape, what,
-              "tensors of different sizes or types")
-        if name == "Q":
-            p.h_q, p.q, p.q_out = x.shape[1], _rows(what, x, name, d), _rows(what, out, "Qout", d)
-        else:
-            p.h_kv, p.k, p.k_out = x.shape[1], _rows(what, x, name, d), _rows(what, out, "Kout", d)
-    _launch(what, dev, load_library().pbs_rope, ctypes.byref(p), freq.data_ptr(), positions.data_ptr(), _addr(Q), _addr(K),
-            _addr(Qout), _addr(Kout))
+        if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != d or out.shape != t.shape or t.dtype != dt or out.dtype != dt:
+            _refuse(what, "tensors of different sizes or types")
+        heads[k] = t.shape[1]
+        strides += _rows(what, t) + _rows(what, out)
+        places.append((t.data_ptr(), out.data_ptr()))
+    p = _ROPE(tokens, heads[0], heads[1], d, 2 * freq.shape[0], ROPE_LAYOUTS[layout], _DTYPE_CODES.get(dt, -1), magnitude,
+              ROPE_TRANSPOSE if transpose else 0, strides[0], strides[1], strides[4], strides[5], strides[2], strides[3],
+              strides[6], strides[7])
+    _launch(what, dev, (_lib or load_library()).pbs_rope, p, freq.data_ptr(), positions.data_ptr(), places[0][0], places[1][0],
+            places[0][1], places[1][1])
     return Qout, Kout
 
 
@@ -455,22 +469,25 @@ class Cache:
     rows' factors k_scale and v_scale [pages, h_kv, page] float32)."""
 
     def __init__(self, K, V, k_scale=None, v_scale=None):
-        what = "pbs_cache"
-        self.device = _device_of(what, K, V, k_scale, v_scale)
-        _need(K.dim() == 4 and K.shape == V.shape and K.dtype == V.dtype, what, "K and V have to be [pages, h_kv, page, d] alike")
-        _need(K.is_contiguous() and V.is_contiguous(), what, "pages have to be contiguous")
-        _need(K.dtype in _DTYPE_CODES and K.dtype != torch.float32, what, "a cache holds bf16, float8_e4m3fn or int8")
-        if K.dtype == torch.bfloat16:
+        what, dt = "pbs_cache", K.dtype
+        dev = K.get_device()
+        _same_device(what, dev, V, k_scale, v_scale)
+        if K.dim() != 4 or K.shape != V.shape or dt != V.dtype or not K.is_contiguous() or not V.is_contiguous():
+            _refuse(what, "K and V have to be contiguous [pages, h_kv, page, d] alike")
+        code = _DTYPE_CODES.get(dt, PBS_F32)
+        if code == PBS_F32:
+            _refuse(what, "a cache holds bf16, float8_e4m3fn or int8")
+        if code == PBS_BF16:
             k_scale = v_scale = None
         else:
             for f in (k_scale, v_scale):
-                _need(f is not None and f.dtype == torch.float32 and f.shape == K.shape[:3] and f.is_contiguous(), what,
-                      "factors have to be contiguous float32 [pages, h_kv, page]")
-        self.K, self.V, self.k_scale, self.v_scale = K, V, k_scale, v_scale
+                if f is None or f.dtype != torch.float32 or f.shape != K.shape[:3] or not f.is_contiguous():
+                    _refuse(what, "factors have to be contiguous float32 [pages, h_kv, page]")
+        self.K, self.V, self.k_scale, self.v_scale, self.dev = K, V, k_scale, v_scale, dev
         self.pages, self.h_kv, self.page, self.d = K.shape
-        self.c = pbs_cache(self.pages, self.page, self.h_kv, self.d, _DTYPE_CODES[K.dtype], K.data_ptr(), V.data_ptr(),
-                           _addr(k_scale), _addr(v_scale))
-        self.ref = ctypes.byref(self.c)
+        # what the library gets; the tensors above keep the memory
+        self.c = _CACHE(self.pages, self.page, self.h_kv, self.d, code, K.data_ptr(), V.data_ptr(),
+                        k_scale.data_ptr() if k_scale is not None else 0, v_scale.data_ptr() if v_scale is not None else 0)
 
     @classmethod
     def alloc(cls, pages, page, h_kv, d, dtype=torch.bfloat16, device="cuda"):
@@ -483,37 +500,43 @@ class Cache:
 
 def cache_write(cache, K, V, slots):
     """Rows K, V [tokens, h_kv, d] into the slots [tokens] of the cache; a slot outside it is passed over."""
-    what = "pbs_cache_write"
-    dev = _device_of(what, cache.K, K, V, slots)
-    _need(K.shape == V.shape and K.dtype == V.dtype and K.dim() == 3 and K.shape[1:] == (cache.h_kv, cache.d), what,
-          "K and V have to be [tokens, h_kv, d] alike")
-    _ints(what, slots, "slots", K.shape[0])
-    _launch(what, dev, load_library().pbs_cache_write, cache.ref, _DTYPE_CODES.get(K.dtype, -1), K.shape[0], K.data_ptr(),
-            _rows(what, K, "K"), V.data_ptr(), _rows(what, V, "V"), slots.data_ptr())
+    what, dev = "pbs_cache_write", cache.dev
+    _same_device(what, dev, K, V, slots)
+    if K.dim() != 3 or K.shape != V.shape or K.dtype != V.dtype or K.shape[1] != cache.h_kv or K.shape[2] != cache.d:
+        _refuse(what, "K and V have to be [tokens, h_kv, d] alike")
+    n = K.shape[0]
+    _ints(what, slots, "slots", n)
+    _launch(what, dev, (_lib or load_library()).pbs_cache_write, cache.c, _DTYPE_CODES.get(K.dtype, -1), n, K.data_ptr(),
+            _STRIDES(*_rows(what, K)), V.data_ptr(), _STRIDES(*_rows(what, V)), slots.data_ptr())
 
 
 def cache_read(cache, slots, dtype="bf16", K=None, V=None):
     """(K, V) [tokens, h_kv, d] that the slots stand for; zeros for a slot outside the cache.  Into K and V where given."""
-    what = "pbs_cache_read"
-    dev = _device_of(what, cache.K, slots, K, V)
-    _ints(what, slots, "slots", slots.numel())
-    dt = {"bf16": torch.bfloat16, "f32": torch.float32}.get(dtype, dtype)
-    shape = (slots.numel(), cache.h_kv, cache.d)
-    out = [torch.empty(shape, dtype=dt, device=dev) if x is None else x for x in (K, V)]
-    for x in out:
-        _need(tuple(x.shape) == shape and x.dtype == dt, what, "K and V have to be [tokens, h_kv, d] of the type asked for")
-    _launch(what, dev, load_library().pbs_cache_read, cache.ref, _DTYPE_CODES.get(dt, -1), shape[0], slots.data_ptr(),
-            out[0].data_ptr(), _rows(what, out[0], "K"), out[1].data_ptr(), _rows(what, out[1], "V"))
-    return out[0], out[1]
+    what, dev = "pbs_cache_read", cache.dev
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32 if dtype == "f32" else dtype
+    n = slots.numel()
+    _ints(what, slots, "slots", n)
+    shape = (n, cache.h_kv, cache.d)
+    if K is None:
+        K = torch.empty(shape, dtype=dt, device=cache.K.device)
+    if V is None:
+        V = torch.empty(shape, dtype=dt, device=cache.K.device)
+    _same_device(what, dev, slots, K, V)
+    if K.shape != shape or V.shape != shape or K.dtype != dt or V.dtype != dt:
+        _refuse(what, "K and V have to be [tokens, h_kv, d] of the type asked for")
+    _launch(what, dev, (_lib or load_library()).pbs_cache_read, cache.c, _DTYPE_CODES.get(dt, -1), n, slots.data_ptr(),
+            K.data_ptr(), _STRIDES(*_rows(what, K)), V.data_ptr(), _STRIDES(*_rows(what, V)))
+    return K, V
 
 
-def _token_strides(what, x, name):
-    """Strides of a [n_seq, q_len, heads, d] tensor whose first two axes are one axis of tokens."""
-    s, t, h, e = x.stride()
-    _need(x.dim() == 4 and (e == 1 or x.numel() == 0), what, "the features of %s are not consecutive" % name)
-    _need(x.shape[0] <= 1 or x.shape[1] == 1 or s == x.shape[1] * t, what, "the tokens of %s are not evenly spaced" % name)
-    token = t if x.shape[1] > 1 else s if x.shape[0] > 1 else 0
-    return pbs_strides(token, h if x.shape[2] > 1 else 0)
+def _token_strides(what, x):
+    """(token, head) strides of a [n_seq, q_len, heads, d] tensor whose first two axes are one axis of tokens."""
+    (n, q, h, _), (s, t, sh, e) = x.shape, x.stride()
+    if e != 1 and x.numel():
+        _refuse(what, "the features of a tensor are not consecutive")
+    if n > 1 and q > 1 and s != q * t:
+        _refuse(what, "the tokens of a tensor are not evenly spaced")
+    return (t if q > 1 else s if n > 1 else 0, sh if h > 1 else 0)
 
 
 def decode_attn(cache, Q, page_table, lens, max_len=None, prefix_pages=None, prefix_len=0, scale=0.0, O=None, lse=None,
@@ -521,36 +544,41 @@ def decode_attn(cache, Q, page_table, lens, max_len=None, prefix_pages=None, pre
     """Attention of Q [n_seq, q_len, h_q, d], the newest tokens of n_seq sequences, over their cached keys: page_table
     [n_seq, max_pages], lens [n_seq] own keys (the new ones among them, at most max_len), behind prefix_len keys of
     prefix_pages that all sequences share.  O like Q; (O, lse [n_seq, q_len, h_q]) with want_lse."""
-    what = "pbs_decode_attn"
-    dev = _device_of(what, cache.K, Q, page_table, lens, prefix_pages, O, lse, ws)
-    _need(Q.dim() == 4 and Q.shape[3] == cache.d, what, "Q has to be [n_seq, q_len, h_q, d]")
-    n, q_len, h_q, d = Q.shape
-    _need(page_table.dim() == 2, what, "page_table has to be [n_seq, max_pages]")
-    _ints(what, page_table, "page_table", n, page_table.shape[1])
+    what, dev, lib = "pbs_decode_attn", cache.dev, _lib or load_library()
+    if Q.dim() != 4 or Q.shape[3] != cache.d or page_table.dim() != 2:
+        _refuse(what, "Q has to be [n_seq, q_len, h_q, d] and page_table [n_seq, max_pages]")
+    n, q_len, h_q, _ = Q.shape
+    max_pages = page_table.shape[1]
+    _ints(what, page_table, "page_table", n, max_pages)
     _ints(what, lens, "lens", n)
     if prefix_len:
-        _need(prefix_pages is not None, what, "prefix_len without prefix_pages")
+        if prefix_pages is None or prefix_pages.numel() < -(-prefix_len // cache.page):
+            _refuse(what, "prefix_pages is shorter than prefix_len")
         _ints(what, prefix_pages, "prefix_pages", prefix_pages.numel())
-        _need(prefix_pages.numel() >= -(-prefix_len // cache.page), what, "prefix_pages is shorter than prefix_len")
+    else:
+        prefix_pages = None
     if max_len is None:
-        max_len = page_table.shape[1] * cache.page
+        max_len = max_pages * cache.page
     if O is None:
-        O = torch.empty(Q.shape, dtype=Q.dtype, device=dev)
-    _need(O.shape == Q.shape and O.dtype == Q.dtype, what, "O has to be like Q")
-    if lse is None and want_lse:
-        lse = torch.empty((n, q_len, h_q), dtype=torch.float32, device=dev)
-    if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (n, q_len, h_q), what,
-              "lse has to be contiguous float32 [n_seq, q_len, h_q]")
-    p = pbs_decode_problem(n, q_len, h_q, page_table.shape[1], max_len, prefix_len, _DTYPE_CODES.get(Q.dtype, -1), scale,
-                           _token_strides(what, Q, "Q"), _token_strides(what, O, "O"))
-    ref, lib = ctypes.byref(p), load_library()
-    need = lib.pbs_decode_workspace_bytes(ref, cache.ref)
+        O = torch.empty_like(Q)
+    elif O.shape != Q.shape or O.dtype != Q.dtype:
+        _refuse(what, "O has to be like Q")
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((n, q_len, h_q), dtype=torch.float32, device=Q.device)
+    elif lse.dtype != torch.float32 or lse.shape != (n, q_len, h_q) or not lse.is_contiguous():
+        _refuse(what, "lse has to be contiguous float32 [n_seq, q_len, h_q]")
+    p = _DECODE(n, q_len, h_q, max_pages, max_len, prefix_len, _DTYPE_CODES.get(Q.dtype, -1), scale, *_token_strides(what, Q),
+                *_token_strides(what, O))
+    need = lib.pbs_decode_workspace_bytes(p, cache.c)
     if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    _launch(what, dev, lib.pbs_decode_attn, ref, cache.ref, Q.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
-            _addr(prefix_pages), O.data_ptr(), _addr(lse), _addr(ws), 0 if ws is None else ws.numel() * ws.element_size())
-    return (O, lse) if lse is not None else O
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+    _same_device(what, dev, Q, O, page_table, lens, prefix_pages, lse, ws)
+    _launch(what, dev, lib.pbs_decode_attn, p, cache.c, Q.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
+            prefix_pages.data_ptr() if prefix_pages is not None else None, O.data_ptr(),
+            lse.data_ptr() if lse is not None else None, ws.data_ptr() if ws is not None else None,
+            ws.numel() * ws.element_size() if ws is not None else 0)
+    return O if lse is None else (O, lse)
 
 
 PROMPT_CAUSAL = 1
@@ -560,32 +588,35 @@ def prompt_attn(Q, K, V, cu_q, cu_k=None, causal=True, scale=0.0, O=None, lse=No
     """Attention of packed prompts: Q [total_q, h_q, d] over K, V [total_k, h_kv, d], sequence i being the rows cu_q[i] ..
     cu_q[i + 1] - 1 and cu_k[i] .. cu_k[i + 1] - 1 (cu_q where cu_k is None).  Causal: the last query sees the last key.
     O like Q, its rows of no sequence as they were (new memory is not cleared); (O, lse [total_q, h_q]) with want_lse."""
-    what = "pbs_prompt_attn"
-    dev = _device_of(what, Q, K, V, cu_q, cu_k, O, lse)
-    _need(Q.dim() == 3 and K.dim() == 3 and K.shape == V.shape and K.shape[2] == Q.shape[2], what,
-          "Q, K and V have to be [rows, heads, d], K and V alike")
-    _need(Q.dtype == K.dtype == V.dtype, what, "tensors of different types")
+    what, dev, dt = "pbs_prompt_attn", Q.get_device(), Q.dtype
+    if Q.dim() != 3 or K.dim() != 3 or K.shape != V.shape or K.shape[2] != Q.shape[2] or K.dtype != dt or V.dtype != dt:
+        _refuse(what, "Q, K and V have to be [rows, heads, d] of one type, K and V alike")
     total, h_q, d = Q.shape
+    total_k, h_kv, _ = K.shape
     if cu_k is None:
         cu_k = cu_q
-        _need(K.shape[0] == total, what, "without cu_k there is a key to every query")
-    _need(cu_q.dim() == 1 and cu_q.numel() >= 1, what, "cu_q has to be [n_seq + 1]")
-    _ints(what, cu_q, "cu_q", cu_q.numel())
-    _ints(what, cu_k, "cu_k", cu_q.numel())
+        if total_k != total:
+            _refuse(what, "without cu_k there is a key to every query")
+    n = cu_q.numel()
+    if n < 1:
+        _refuse(what, "cu_q has to be [n_seq + 1]")
+    _ints(what, cu_q, "cu_q", n)
+    _ints(what, cu_k, "cu_k", n)
     if O is None:
-        O = torch.empty(Q.shape, dtype=Q.dtype, device=dev)
-    _need(O.shape == Q.shape and O.dtype == Q.dtype, what, "O has to be like Q")
-    if lse is None and want_lse:
-        lse = torch.empty((total, h_q), dtype=torch.float32, device=dev)
-    if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (total, h_q), what,
-              "lse has to be contiguous float32 [total_q, h_q]")
-    p = pbs_prompt_problem(cu_q.numel() - 1, total, K.shape[0], h_q, K.shape[1], d, _DTYPE_CODES.get(Q.dtype, -1), scale,
-                           PROMPT_CAUSAL if causal else 0, _rows(what, Q, "Q"), _rows(what, K, "K"), _rows(what, V, "V"),
-                           _rows(what, O, "O"))
-    _launch(what, dev, load_library().pbs_prompt_attn, ctypes.byref(p), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-            cu_q.data_ptr(), cu_k.data_ptr(), O.data_ptr(), _addr(lse))
-    return (O, lse) if lse is not None else O
+        O = torch.empty_like(Q)
+    elif O.shape != Q.shape or O.dtype != dt:
+        _refuse(what, "O has to be like Q")
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((total, h_q), dtype=torch.float32, device=Q.device)
+    elif lse.dtype != torch.float32 or lse.shape != (total, h_q) or not lse.is_contiguous():
+        _refuse(what, "lse has to be contiguous float32 [total_q, h_q]")
+    _same_device(what, dev, K, V, cu_q, cu_k, O, lse)
+    p = _PROMPT(n - 1, total, total_k, h_q, h_kv, d, _DTYPE_CODES.get(dt, -1), scale, PROMPT_CAUSAL if causal else 0,
+                *_rows(what, Q), *_rows(what, K), *_rows(what, V), *_rows(what, O))
+    _launch(what, dev, (_lib or load_library()).pbs_prompt_attn, p, Q.data_ptr(), K.data_ptr(), V.data_ptr(), cu_q.data_ptr(),
+            cu_k.data_ptr(), O.data_ptr(), lse.data_ptr() if lse is not None else None)
+    return O if lse is None else (O, lse)
 
 
 class Pipeline:

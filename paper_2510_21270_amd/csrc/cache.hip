@@ -1,9 +1,9 @@
 // pbs_cache_write, pbs_cache_read: the rows of a paged key/value cache.
 //
-// A row (token, kv head) is d features: 8 to a lane, 8 or 16 lanes.  Writing in 8 bits finds the row's largest magnitude
-// across these lanes and divides by f = max(largest / M, 2^-126); both divisions are IEEE fp32, so that what is held is
-// the same wherever it is formed.  Magnitudes are compared as bit patterns: infinite and NaN features are the
-// largest ones and show.  Bytes bound both directions.
+// A row (token, kv head) is d features: 8 to a lane, 8 or 16 lanes; a thread has its piece of the K row and of the V row.
+// Writing in 8 bits finds a row's largest magnitude across these lanes and divides by f = max(largest / M, 2^-126); both
+// divisions are IEEE fp32, so that what is held is the same wherever it is formed.  Magnitudes are compared as bit
+// patterns: infinite and NaN features are the largest ones and show.  Bytes bound both directions.
 #include "pbs_host.h"
 #include "serving.h"
 
@@ -65,7 +65,38 @@ __device__ __forceinline__ void held_to_float(const Held8 &q, float (&x)[8])
     }
 }
 
-// blockIdx.y: 0 = K, 1 = V.
+// x / f, rounded as IEEE division does, by the reciprocal y = 1 / f and two corrections: with y rounded correctly and q within a
+// step of the quotient, x - q f is exact and q + y (x - q f) rounds correctly (Markstein 1990).  The first correction brings q
+// there.  Exact as long as x - q f does not fall below the smallest numbers, which is what `small` rows are kept away from.
+__device__ __forceinline__ float quotient(float x, float f, float y)
+{
+    float q = x * y;
+    q = __builtin_fmaf(__builtin_fmaf(-q, f, x), y, q);
+    return __builtin_fmaf(__builtin_fmaf(-q, f, x), y, q);
+}
+
+// Eight features of a row in 8 bits, and the row's factor.
+template <int DTYPE>
+__device__ __forceinline__ Held8 hold8(const float (&x)[8], int lanes, float &factor)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int o = lanes >> 1; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+    const bool finite = most < 0x7f800000u, small = most < 0x21800000u;        // 2^-60
+    const float f = fmaxf(__uint_as_float(most) / (DTYPE == PBS_E4M3 ? 448.0f : 127.0f), kTinyFactor), y = 1.0f / f;
+    float q[8];
+    if (__any(small || !finite)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = finite ? x[i] / f : 0.0f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = quotient(x[i], f, y);
+    }
+    factor = finite ? f : __uint_as_float(0x7fc00000u);
+    return round_to_held<DTYPE>(q);
+}
+
 template <typename E, int DTYPE>
 __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheArgs a, const E *__restrict__ K,
                                                                     const E *__restrict__ V, void *__restrict__ Kc,
@@ -78,32 +109,27 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheArgs a,
     if (row >= a.rows) return;                             // whole rows leave together
     const int t = row / a.h_kv, h = row - t * a.h_kv;
     const int s = a.slot[t];
+    float k[8], v[8];
+    load8(K + (int64_t)t * a.x[0].token + (int64_t)h * a.x[0].head + 8 * lane, k);
+    load8(V + (int64_t)t * a.x[1].token + (int64_t)h * a.x[1].head + 8 * lane, v);
     if (s < 0 || s >= a.slots) return;
-    const bool is_v = blockIdx.y != 0;
-    const pbs_strides &st = a.x[is_v ? 1 : 0];
-    const E *src = (is_v ? V : K) + (int64_t)t * st.token + (int64_t)h * st.head + 8 * lane;
-    const int64_t to = cache_row(s, h, a.h_kv, a.page_log);
-    float x[8];
-    load8(src, x);
+    const int64_t to = cache_row(s, h, a.h_kv, a.page_log), place = (to << a.d_log) + 8 * lane;
     if constexpr (DTYPE == PBS_BF16) {
-        store8(static_cast<bf16_t *>(is_v ? Vc : Kc) + (to << a.d_log) + 8 * lane, x);
+        store8(static_cast<bf16_t *>(Kc) + place, k);
+        store8(static_cast<bf16_t *>(Vc) + place, v);
     } else {
-        uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-        for (int o = lanes >> 1; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
-        const bool finite = most < 0x7f800000u;
-        const float f = fmaxf(__uint_as_float(most) / (DTYPE == PBS_E4M3 ? 448.0f : 127.0f), kTinyFactor);
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = finite ? x[i] / f : 0.0f;
-        const Held8 q = round_to_held<DTYPE>(y);
-        uint2 *dst = reinterpret_cast<uint2 *>(static_cast<uint8_t *>(is_v ? Vc : Kc) + (to << a.d_log) + 8 * lane);
-        *dst = make_uint2(q.lo, q.hi);
-        if (lane == 0) (is_v ? vf : kf)[to] = finite ? f : __uint_as_float(0x7fc00000u);
+        float fk, fv;
+        const Held8 qk = hold8<DTYPE>(k, lanes, fk), qv = hold8<DTYPE>(v, lanes, fv);
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(Kc) + place) = make_uint2(qk.lo, qk.hi);
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(Vc) + place) = make_uint2(qv.lo, qv.hi);
+        if (lane == 0) {
+            kf[to] = fk;
+            vf[to] = fv;
+        }
     }
 }
 
+// blockIdx.y: 0 = K, 1 = V.
 template <typename E, int DTYPE>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheArgs a, E *__restrict__ K, E *__restrict__ V,
                                                                    const void *__restrict__ Kc,
@@ -156,9 +182,9 @@ inline pbs_status cache_args(const pbs_cache *c, int32_t dtype, int32_t tokens, 
     return PBS_OK;
 }
 
-inline dim3 cache_grid(const CacheArgs &a)
+inline dim3 cache_grid(const CacheArgs &a, int y)
 {
-    return dim3((unsigned)((((int64_t)a.rows << (a.d_log - 3)) + kCacheThreads - 1) / kCacheThreads), 2);
+    return dim3((unsigned)((((int64_t)a.rows << (a.d_log - 3)) + kCacheThreads - 1) / kCacheThreads), y);
 }
 
 template <typename E>
@@ -167,7 +193,7 @@ pbs_status write_rows(const pbs_cache *c, const CacheArgs &a, const void *K, con
     const E *k = static_cast<const E *>(K), *v = static_cast<const E *>(V);
     auto kernel = c->dtype == PBS_BF16 ? cache_write_kernel<E, PBS_BF16>
                   : c->dtype == PBS_E4M3 ? cache_write_kernel<E, PBS_E4M3> : cache_write_kernel<E, PBS_I8>;
-    return launch(kernel, cache_grid(a), dim3(kCacheThreads), 0, s, a, k, v, c->K, c->V, c->k_scale, c->v_scale);
+    return launch(kernel, cache_grid(a, 1), dim3(kCacheThreads), 0, s, a, k, v, c->K, c->V, c->k_scale, c->v_scale);
 }
 
 template <typename E>
@@ -176,7 +202,7 @@ pbs_status read_rows(const pbs_cache *c, const CacheArgs &a, void *K, void *V, h
     E *k = static_cast<E *>(K), *v = static_cast<E *>(V);
     auto kernel = c->dtype == PBS_BF16 ? cache_read_kernel<E, PBS_BF16>
                   : c->dtype == PBS_E4M3 ? cache_read_kernel<E, PBS_E4M3> : cache_read_kernel<E, PBS_I8>;
-    return launch(kernel, cache_grid(a), dim3(kCacheThreads), 0, s, a, k, v, static_cast<const void *>(c->K),
+    return launch(kernel, cache_grid(a, 2), dim3(kCacheThreads), 0, s, a, k, v, static_cast<const void *>(c->K),
                   static_cast<const void *>(c->V), static_cast<const float *>(c->k_scale),
                   static_cast<const float *>(c->v_scale));
 }

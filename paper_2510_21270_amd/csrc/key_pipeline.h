@@ -522,9 +522,10 @@ __device__ __forceinline__ void clear(State<D> &st)
 
 // Keys of tiles 0 .. tiles - 1 (at least one), of which the wave's rows all see those below `all`.  True where the result does not
 // stand: values that are not finite, or a row that sees keys and has no sum.
-template <int D, bool F, class SRC>
-__device__ __forceinline__ bool all_tiles(State<D> &st, const bf16x8 (&q)[2][D / 16], const int (&sees)[2], int all, int tiles,
-                                          float c2, const SRC &src, const Offsets<D> &off, Stage<D, F> &sg0, Stage<D, F> &sg1,
+// load_queries brings the rows' queries into q, behind the first tiles' loads.  At the end no load into LDS is left, of either wave.
+template <int D, bool F, class SRC, class LQ>
+__device__ __forceinline__ bool all_tiles(State<D> &st, bf16x8 (&q)[2][D / 16], LQ load_queries, const int (&sees)[2], int all,
+                                          int tiles, float c2, const SRC &src, const Offsets<D> &off, Stage<D, F> &sg0, Stage<D, F> &sg1,
                                           Stage<D, F> &sg2, Stage<D, F> &sg3, int wave, int lane)
 {
     const int h = lane >> 5;
@@ -536,6 +537,7 @@ __device__ __forceinline__ bool all_tiles(State<D> &st, const bf16x8 (&q)[2][D /
     issue_factors(sg0, src, 0, wave, lane);
     issue_factors(sg1, src, 1, wave, lane);
     issue_factors(sg2, src, 2, wave, lane);
+    load_queries();
     meet();
     floatx16 sa[2], sb[2];
     bf16x8 kf[D / 16], pa[2][2], pb[2][2];
@@ -583,6 +585,7 @@ __device__ __forceinline__ bool all_tiles(State<D> &st, const bf16x8 (&q)[2][D /
         if (t + 4 >= tiles) break;                         // (ways out between the four cost 300 spilled registers and more)
     }
     drain<D>(st, pa, sg0, off);
+    meet();
     float zero = 0.0f;                                     // NaN if a value of O^T is not finite
     bool bad = false;
 #pragma unroll
@@ -596,6 +599,31 @@ __device__ __forceinline__ bool all_tiles(State<D> &st, const bf16x8 (&q)[2][D /
         zero = __builtin_fmaf(l, 0.0f, zero);
     }
     return bad || zero != 0.0f;
+}
+
+// Rows of 32 queries out of O^T (lane (n, h), value x of tile dt: feature 32 dt + 8 (x / 4) + 4 h + x % 4 of query n) through
+// LDS, so that a store instruction writes whole rows: make() turns four features into elements E, put(row, piece, value) gets 16
+// bytes of a row.  room: 32 rows of LDS of the wave's own, at most a stage; piece p of row n lies at place p ^ n.
+template <int D, typename E, class MAKE, class PUT>
+__device__ __forceinline__ void rows_out(const State<D> &st, int nt, unsigned char *room, int lane, MAKE make, PUT put)
+{
+    constexpr int kRowB = D * (int)sizeof(E), kPieces = kRowB / 16, kGroup = 4 * (int)sizeof(E);
+    typedef E ex4 __attribute__((ext_vector_type(4)));
+    const int n = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const floatx16 &o = st.o[dt][nt];
+            const int at = (8 * dt + 2 * x + h) * kGroup;
+            *reinterpret_cast<ex4 *>(room + n * kRowB + ((at >> 4 ^ (n & (kPieces - 1))) << 4) + (at & 15)) =
+                make(floatx4{o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]});
+        }
+#pragma unroll 2
+    for (int y = 0; y < 32 * kPieces / 64; ++y) {
+        const int row = (64 * y + lane) / kPieces, piece = lane % kPieces;
+        put(row, piece, *reinterpret_cast<const uintx4 *>(room + row * kRowB + ((piece ^ (row & (kPieces - 1))) << 4)));
+    }
 }
 
 }  // namespace prompt

@@ -10,8 +10,9 @@ namespace pbs {
 namespace prompt {
 
 // Tiles of a part from the pages of a cache.  held: the pages of the part's 32 tiles in a wave's lanes, two to a tile.  The halves of a
-// tile have a descriptor each, which ends with the keys that exist: what lies behind them reads as zeros.
-template <int D>
+// tile have a descriptor each where a page is no more (HALVES), which ends with the keys that exist: what lies behind them reads as
+// zeros.
+template <int D, bool HALVES>
 struct Pages {
     const bf16_t *pool;
     int held, count, begin, page_log, h, h_kv;
@@ -26,16 +27,22 @@ struct Pages {
         const bf16_t *base = pool + (((((int64_t)max(page, 0)) * h_kv + h) << page_log) + place - 16 * u) * D;
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(base), 0, page >= 0 && rows > 16 * u ? rows * D * 2 : 0, 0x00020000);
     }
-    __device__ __forceinline__ At at(int t) const { return {half(t, 0), half(t, 1)}; }
+    __device__ __forceinline__ At at(int t) const
+    {
+        At w;
+        w.lo = half(t, 0);
+        if constexpr (HALVES) w.hi = half(t, 1);
+        return w;
+    }
     __device__ __forceinline__ void load(unsigned char *dst, int c, const At &w, const Offsets<D> &off) const
     {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(c < Offsets<D>::kLoads / 2 ? w.lo : w.hi, (lptr_t)(dst + c * 1024), 16, off.from[c], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(!HALVES || c < Offsets<D>::kLoads / 2 ? w.lo : w.hi, (lptr_t)(dst + c * 1024), 16, off.from[c], 0, 0, 0);
     }
     __device__ __forceinline__ void load_factors(float *, int, int) const {}
 };
 
-// LINE: the keys lie in order as bf16 with factors beside them.
-template <int D, bool LINE>
+// LINE: the keys lie in order as bf16 with factors beside them.  HALVES: in pages of 16.
+template <int D, bool LINE, bool HALVES>
 __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void prefix_kernel(DecodeArgs a, bool single)
 {
     __shared__ Stage<D, LINE> sg0, sg1, sg2, sg3;
@@ -53,12 +60,16 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         if (held >= a.pages) held = -1;
         bad = held < 0;
     }
+    // row / r: the workgroup's first row by a division, its 128 rows by 1 / r, at least 1 / 2 r off the next whole number
+    const int t0 = row0 / a.r, rest = row0 - t0 * a.r;
+    const float inv_r = 1.0f / (float)a.r;
+    auto token_of = [&](int row) { return t0 + (int)(((float)(row - row0 + rest) + 0.5f) * inv_r); };
     bf16x8 q[2][D / 16];
     const int sees[2] = {count, count};
     auto load_queries = [&]() {
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-            const int row = min(row0 + wave * 64 + 32 * nt + n, rows - 1), t = row / a.r;
+            const int row = min(row0 + wave * 64 + 32 * nt + n, rows - 1), t = token_of(row);
             const bf16_t *src = a.Q + (int64_t)t * a.q.token + (int64_t)(kv * a.r + row - t * a.r) * a.q.head + 8 * h;
 #pragma unroll
             for (int x = 0; x < D / 16; ++x) q[nt][x] = *reinterpret_cast<const bf16x8 *>(src + 16 * x);
@@ -75,40 +86,50 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             s.factors = __builtin_amdgcn_make_buffer_rsrc((wave == 0 ? a.line_kf : a.line_vf) + first, 0, s.factors_size, 0x00020000);
             return s;
         } else {
-            return Pages<D>{reinterpret_cast<const bf16_t *>(wave == 0 ? a.K : a.V), held, count, begin, a.page_log, kv, a.h_kv};
+            return Pages<D, HALVES>{reinterpret_cast<const bf16_t *>(wave == 0 ? a.K : a.V), held, count, begin, a.page_log, kv, a.h_kv};
         }
     };
+    unsigned char *const room = reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1);
     auto store = [&](const State<D> &st) {
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-            const int row = row0 + wave * 64 + 32 * nt + n;
-            const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64);
-            if (row >= rows) continue;
-            const int t = row / a.r, head = kv * a.r + row - t * a.r;
-            const int64_t out = (int64_t)t * a.h_q + head, at = (int64_t)part * a.n_seq * a.q_len * a.h_q + out;
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const floatx16 &o = st.o[dt][nt];
-                    const floatx4 v = {o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]};
-                    const int f = 32 * dt + 8 * x + 4 * h;
-                    if (single)
-                        *reinterpret_cast<bf16x4 *>(a.O + (int64_t)t * a.o.token + (int64_t)head * a.o.head + f) =
-                            __builtin_convertvector(l == 0.0f ? floatx4{0} : v * inv, bf16x4);
-                    else
-                        *reinterpret_cast<floatx4 *>(a.part_o + at * D + f) = v;
+            const int first = row0 + wave * 64 + 32 * nt, row = first + n;
+            const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64), inv = l == 0.0f ? 0.0f : 1.0f / l;
+            auto out_of = [&](int y, int &t, int &head) {
+                t = token_of(y);
+                head = kv * a.r + y - t * a.r;
+                return (int64_t)t * a.h_q + head;
+            };
+            const int64_t parts = (int64_t)part * a.n_seq * a.q_len * a.h_q;
+            int t, head;
+            if (single) {
+                rows_out<D, bf16_t>(st, nt, room, lane,
+                                    [&](floatx4 v) { return __builtin_convertvector(l == 0.0f ? floatx4{0} : v * inv, bf16x4); },
+                                    [&](int x, int piece, uintx4 v) {
+                                        int ot, oh;
+                                        out_of(first + x, ot, oh);
+                                        if (first + x < rows)
+                                            *reinterpret_cast<uintx4 *>(a.O + (int64_t)ot * a.o.token + (int64_t)oh * a.o.head + 8 * piece) = v;
+                                    });
+                if (row < rows && h == 0 && a.lse) {
+                    const int64_t out = out_of(row, t, head);
+                    a.lse[out] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
                 }
-            if (h == 0 && !single) {
-                a.part_ml[2 * at] = st.m[nt];
-                a.part_ml[2 * at + 1] = l;
-            } else if (h == 0 && a.lse) {
-                a.lse[out] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            } else {
+                rows_out<D, float>(st, nt, room, lane, [&](floatx4 v) { return v; },
+                                   [&](int x, int piece, uintx4 v) {
+                                       int ot, oh;
+                                       const int64_t out = out_of(first + x, ot, oh);
+                                       if (first + x < rows) *reinterpret_cast<uintx4 *>(a.part_o + (parts + out) * D + 4 * piece) = v;
+                                   });
+                if (row < rows && h == 0) {
+                    const int64_t at = parts + out_of(row, t, head);
+                    a.part_ml[2 * at] = st.m[nt];
+                    a.part_ml[2 * at + 1] = l;
+                }
             }
         }
     };
-    load_queries();
     const auto src = source();
     const Offsets<D> off = offsets<D>(wave, lane, D * 2);
     const unsigned long long missing = __ballot(bad);      // sixteens of keys in no page
@@ -116,10 +137,10 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     {
         State<D> st;
         clear(st);
-        bad = all_tiles<D, LINE>(st, q, sees, count, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane) || missing != 0;
-        store(st);
+        bad = all_tiles<D, LINE>(st, q, load_queries, sees, count, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane) || missing != 0;
+        store(st);                                         // (nobody waits for the stores)
     }
-    meet();
+    __syncthreads();
     if (__any(bad) && lane == 0) bad_rows = 1;
     __syncthreads();
     if (__builtin_expect(bad_rows != 0, 0)) {
@@ -133,6 +154,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             meet();
             whole_tile<D, LINE>(st, sg0, off, q, sees, t * KS, (int)(~missing >> (2 * t)) & 3, a.c2, h);
         }
+        __syncthreads();
         store(st);
     }
 }
@@ -166,12 +188,16 @@ pbs_status launch_prefix(const DecodeArgs &a, int dtype, int d, bool single, hip
 {
     using namespace prompt;
     const dim3 grid(a.h_kv, a.p_row_tiles, a.p_parts), block(128);
-    if (dtype == PBS_BF16) return launch(d == 128 ? prefix_kernel<128, false> : prefix_kernel<64, false>, grid, block, 0, s, a, single);
+    if (dtype == PBS_BF16) {
+        auto kernel = d == 128 ? (a.page_log == 4 ? prefix_kernel<128, false, true> : prefix_kernel<128, false, false>)
+                               : (a.page_log == 4 ? prefix_kernel<64, false, true> : prefix_kernel<64, false, false>);
+        return launch(kernel, grid, block, 0, s, a, single);
+    }
     auto line = d == 128 ? (dtype == PBS_E4M3 ? line_kernel<PBS_E4M3, 128> : line_kernel<PBS_I8, 128>)
                          : (dtype == PBS_E4M3 ? line_kernel<PBS_E4M3, 64> : line_kernel<PBS_I8, 64>);
     const pbs_status st = launch(line, dim3((unsigned)(((int64_t)a.p_room * (d / 8) + 255) / 256), a.h_kv), dim3(256), 0, s, a);
     if (st != PBS_OK) return st;
-    return launch(d == 128 ? prefix_kernel<128, true> : prefix_kernel<64, true>, grid, block, 0, s, a, single);
+    return launch(d == 128 ? prefix_kernel<128, true, false> : prefix_kernel<64, true, false>, grid, block, 0, s, a, single);
 }
 
 }  // namespace pbs

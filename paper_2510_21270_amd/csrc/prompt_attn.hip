@@ -9,7 +9,7 @@ namespace prompt {
 
 struct Args {
     int n_seq, total_q, total_k, h_q, h_kv, r, tokens;     // tokens: of a workgroup's rows
-    float c2;                                              // scale * log2(e)
+    float c2, inv_r;                                       // scale * log2(e); 1 / r
     bool causal;
     pbs_strides q, k, v, o;
     const bf16_t *Q, *K, *V;
@@ -18,69 +18,69 @@ struct Args {
     float *lse;
 };
 
-// Which sequence and which of its tiles workgroup `b` has: the sequences' tiles one behind the other, a sequence's last
-// tile, the longest, first.  Every wave looks for itself.  seq = -1: none is left.
+// Which sequence and which of its tiles workgroup `b` has: the sequences' tiles one behind the other, a sequence's last tile, the
+// longest, first.  (Tiles with the most keys first over all sequences left no long one for the end, but neighbours no longer
+// shared keys in L2: 16 prompts of 33 .. 2048 tokens, 32 / 8 heads, 106 -> 114 us.)  Every wave looks for itself, a lane to a
+// sequence.  seq = -1: none is left.
 struct Place { int seq, tile, q0, len_q, k0, len_k; };
 __device__ __forceinline__ Place find_place(const Args &a, int b, int lane)
 {
     Place p = {-1, 0, 0, 0, 0, 0};
-    int before = 0;
     for (int base = 0; base < a.n_seq; base += 64) {
         const int i = base + lane;
-        int q0 = 0, len = 0;
+        int q0 = 0, len_q = 0, k0 = 0, len_k = 0;
         if (i < a.n_seq) {
             q0 = min(max(a.cu_q[i], 0), a.total_q);
-            len = max(min(max(a.cu_q[i + 1], 0), a.total_q) - q0, 0);
+            len_q = max(min(max(a.cu_q[i + 1], 0), a.total_q) - q0, 0);
+            k0 = min(max(a.cu_k[i], 0), a.total_k);
+            len_k = max(min(max(a.cu_k[i + 1], 0), a.total_k) - k0, 0);
         }
-        const int tiles = (len + a.tokens - 1) / a.tokens;
+        const int tiles = (len_q + a.tokens - 1) / a.tokens;
         int sum = tiles;
+        if (a.n_seq > 1) {
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int other = __shfl_up(sum, o, 64);
-            if (lane >= o) sum += other;
+            for (int o = 1; o < 64; o <<= 1) {
+                const int other = __shfl_up(sum, o, 64);
+                if (lane >= o) sum += other;
+            }
         }
-        const int total = __builtin_amdgcn_readlane(sum, 63);
-        if (b < before + total) {
-            const unsigned long long has = __ballot(b < before + sum);
+        const unsigned long long has = __ballot(i < a.n_seq && b < sum);
+        if (has) {
             const int at = __builtin_ctzll(has);
             p.seq = base + at;
+            p.tile = __builtin_amdgcn_readlane(sum, at) - 1 - b;
             p.q0 = __builtin_amdgcn_readlane(q0, at);
-            p.len_q = __builtin_amdgcn_readlane(len, at);
-            const int in = b - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(tiles, at));
-            p.tile = __builtin_amdgcn_readlane(tiles, at) - 1 - in;
-            const int k0 = min(max(a.cu_k[p.seq], 0), a.total_k);
-            p.k0 = __builtin_amdgcn_readfirstlane(k0);
-            p.len_k = __builtin_amdgcn_readfirstlane(max(min(max(a.cu_k[p.seq + 1], 0), a.total_k) - k0, 0));
+            p.len_q = __builtin_amdgcn_readlane(len_q, at);
+            p.k0 = __builtin_amdgcn_readlane(k0, at);
+            p.len_k = __builtin_amdgcn_readlane(len_k, at);
             return p;
         }
-        before += total;
+        b -= __builtin_amdgcn_readlane(sum, 63);
     }
     return p;
 }
 
-// lane (n, h), value x of O^T tile dt: feature 32 dt + 8 (x / 4) + 4 h + x % 4 of query n
+// row / r for the rows of a workgroup: at least 1 / 2 r off the next whole number
+__device__ __forceinline__ int token_of(const Args &a, int row) { return (int)(((float)row + 0.5f) * a.inv_r); }
+
 template <int D>
-__device__ __forceinline__ void store_rows(const Args &a, const Place &pl, const State<D> &st, int kv, int t0, int rows, int wave, int n, int h)
+__device__ __forceinline__ void store_rows(const Args &a, const Place &pl, const State<D> &st, int kv, int t0, int rows, int wave,
+                                           int lane, unsigned char *room)
 {
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
-        const int row = wave * 64 + 32 * nt + n;
-        const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64);
-        if (row < rows) {
-            const int t = t0 + row / a.r, head = kv * a.r + row % a.r;
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            bf16_t *dst = a.O + (int64_t)(pl.q0 + t) * a.o.token + (int64_t)head * a.o.head + 4 * h;
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const floatx16 &o = st.o[dt][nt];
-                    floatx4 v = floatx4{o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]} * inv;
-                    if (l == 0.0f) v = floatx4{0};
-                    *reinterpret_cast<bf16x4 *>(dst + 32 * dt + 8 * x) = __builtin_convertvector(v, bf16x4);
-                }
-            if (a.lse && h == 0)
-                a.lse[(int64_t)(pl.q0 + t) * a.h_q + head] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        const int row0 = wave * 64 + 32 * nt, row = row0 + (lane & 31);
+        const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64), inv = l == 0.0f ? 0.0f : 1.0f / l;
+        rows_out<D, bf16_t>(st, nt, room, lane,
+                            [&](floatx4 v) { return __builtin_convertvector(l == 0.0f ? floatx4{0} : v * inv, bf16x4); },
+                            [&](int x, int piece, uintx4 v) {
+                                const int y = row0 + x, in = token_of(a, y), head = kv * a.r + y - in * a.r;
+                                if (y < rows)
+                                    *reinterpret_cast<uintx4 *>(a.O + (int64_t)(pl.q0 + t0 + in) * a.o.token + (int64_t)head * a.o.head + 8 * piece) = v;
+                            });
+        if (a.lse && lane < 32 && row < rows) {
+            const int in = token_of(a, row), head = kv * a.r + row - in * a.r;
+            a.lse[(int64_t)(pl.q0 + t0 + in) * a.h_q + head] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
         }
     }
 }
@@ -106,15 +106,18 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const int row = wave * 64 + 32 * nt + n, rc = min(row, rows - 1);
-            const int t = t0 + rc / a.r, head = kv * a.r + rc % a.r;
-            const bf16_t *src = a.Q + (int64_t)(pl.q0 + t) * a.q.token + (int64_t)head * a.q.head + 8 * h;
+            const int in = token_of(a, rc), head = kv * a.r + rc - in * a.r;
+            const bf16_t *src = a.Q + (int64_t)(pl.q0 + t0 + in) * a.q.token + (int64_t)head * a.q.head + 8 * h;
 #pragma unroll
             for (int x = 0; x < D / 16; ++x) q[nt][x] = *reinterpret_cast<const bf16x8 *>(src + 16 * x);
-            sees[nt] = a.causal ? min(max(t + ahead + 1, 0), pl.len_k) : pl.len_k;
         }
     };
-    load_queries();
-    const int last = a.causal ? min(max(t0 + (rows - 1) / a.r + ahead + 1, 0), pl.len_k) : pl.len_k;   // keys that any row sees
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+        const int t = t0 + token_of(a, min(wave * 64 + 32 * nt + n, rows - 1));
+        sees[nt] = a.causal ? min(max(t + ahead + 1, 0), pl.len_k) : pl.len_k;
+    }
+    const int last = a.causal ? min(max(t0 + min(a.tokens, pl.len_q - t0) + ahead, 0), pl.len_k) : pl.len_k;   // keys that any row sees
     const int tiles = (last + KS - 1) / KS;
 
     const pbs_strides &ks = wave == 0 ? a.k : a.v;
@@ -130,13 +133,13 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     bool bad = false;
     if (tiles > 0) {
         const int all = __builtin_amdgcn_readfirstlane(sees[0]);               // the wave's first row sees the fewest keys
-        bad = all_tiles<D, false>(st, q, sees, all, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane);
-        store_rows<D>(a, pl, st, kv, t0, rows, wave, n, h);
+        bad = all_tiles<D, false>(st, q, load_queries, sees, all, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane);
     }
-    meet();                                                // loads past the last tile have landed too
+    store_rows<D>(a, pl, st, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));   // (nobody waits for the stores)
+    __syncthreads();
     if (__any(bad) && lane == 0) bad_rows = 1;
     __syncthreads();
-    if (__builtin_expect(bad_rows != 0 || tiles == 0, 0)) {
+    if (__builtin_expect(bad_rows != 0, 0)) {
         clear(st);
         load_queries();
         for (int t = 0; t < tiles; ++t) {
@@ -145,7 +148,8 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             meet();
             whole_tile<D>(st, sg0, off, q, sees, t * KS, 3, a.c2, h);
         }
-        store_rows<D>(a, pl, st, kv, t0, rows, wave, n, h);
+        __syncthreads();
+        store_rows<D>(a, pl, st, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));
     }
 }
 
@@ -179,6 +183,7 @@ extern "C" pbs_status pbs_prompt_attn(const pbs_prompt_problem *p, const void *Q
     a.n_seq = p->n_seq; a.total_q = p->total_q; a.total_k = p->total_k;
     a.h_q = p->h_q; a.h_kv = p->h_kv; a.r = r; a.tokens = tokens;
     a.c2 = (p->scale > 0.0f ? p->scale : (float)(1.0 / sqrt((double)p->d))) * 1.4426950408889634f;
+    a.inv_r = 1.0f / r;
     a.causal = (p->flags & PBS_PROMPT_CAUSAL) != 0;
     a.q = p->q; a.k = p->k; a.v = p->v; a.o = p->o;
     a.Q = static_cast<const bf16_t *>(Q);

@@ -10,7 +10,7 @@
 namespace pbs {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeTokens = 4;                             // tokens to a workgroup where there are many
+constexpr int kRopeTokens = 8;                             // most tokens to a workgroup
 
 struct RopeArgs {
     int tokens, h_q, heads, d, rot, per_wg;
@@ -117,7 +117,18 @@ extern "C" pbs_status pbs_rope(const pbs_rope_problem *p, const double *freq, co
 
     RopeArgs a;
     a.tokens = p->tokens; a.h_q = p->h_q; a.heads = (int)heads; a.d = p->d; a.rot = p->rot;
-    a.per_wg = p->tokens >= 2048 && heads <= 1024 ? kRopeTokens : 1;
+    // As many tokens to a workgroup as fill the threads' last round best (32 + 8 heads of 128: 4, five full rounds), while there
+    // are workgroups for every compute unit several times over.
+    a.per_wg = 1;
+    double full = 0.0;
+    for (int n = 1; n <= kRopeTokens && p->tokens >= 1024 * n && heads * n <= 4096; ++n) {
+        const long long items = n * heads * (p->d / 16), rounds = (items + kRopeThreads - 1) / kRopeThreads;
+        const double share = (double)items / (double)(rounds * kRopeThreads);
+        if (share > full + 0.02) {
+            full = share;
+            a.per_wg = n;
+        }
+    }
     a.head_magic = (unsigned)((0x100000000ull + heads - 1) / heads);
     a.magnitude = p->magnitude == 0.0f ? 1.0f : p->magnitude;
     a.sign = (p->flags & PBS_ROPE_TRANSPOSE) ? -1.0f : 1.0f;

@@ -41,7 +41,7 @@ def _wait_states(line):
 
 
 def test_operands_are_in_place_and_results_are_left_alone(kernels):
-    assert len(kernels) == 6
+    assert len(kernels) == 8
     for name, lines in kernels.items():
         seen = 0
         for k, line in enumerate(lines):

@@ -21,8 +21,8 @@ FAKE = ctypes.c_void_p(4096)                               # never dereferenced:
 ODD = ctypes.c_void_p(4096 + 8)
 
 
-def _strides(tokens, heads, d):
-    return b.pbs_strides(heads * d, d)
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
 
 
 def _rope(**kw):
@@ -125,10 +125,10 @@ def test_cache_refusals(lib):
     s = b.pbs_strides(128, 64)
 
     def write(c=_cache(), dtype=1, tokens=4, K=FAKE, k=s, V=FAKE, v=s, slots=FAKE):
-        return lib.pbs_cache_write(ctypes.byref(c) if c is not None else None, dtype, tokens, K, k, V, v, slots, None)
+        return lib.pbs_cache_write(_ref(c), dtype, tokens, K, _ref(k), V, _ref(v), slots, None)
 
     def read(c=_cache(), dtype=1, tokens=4, slots=FAKE, K=FAKE, k=s, V=FAKE, v=s):
-        return lib.pbs_cache_read(ctypes.byref(c) if c is not None else None, dtype, tokens, slots, K, k, V, v, None)
+        return lib.pbs_cache_read(_ref(c), dtype, tokens, slots, K, _ref(k), V, _ref(v), None)
 
     for call in (write, read):
         assert call(c=None) == 1 and call(slots=None) == 1
@@ -175,6 +175,23 @@ def test_decode_refusals(lib):
     assert call(p, ws=None) == 1 and call(p, n=need - 1) == 4 and call(p, ws=ODD) == 4
     assert lib.pbs_decode_workspace_bytes(ctypes.byref(_decode(max_len=16)), ctypes.byref(_cache())) == 0   # one part
     assert lib.pbs_decode_workspace_bytes(ctypes.byref(_decode(q_len=0)), ctypes.byref(_cache())) == 0
+
+
+def test_packed_arguments_are_the_structures():
+    import struct
+    for made, of, args in ((b._ROPE, b.pbs_rope_problem, tuple(range(1, 8)) + (0.5, 9) + tuple(range(10, 18))),
+                           (b._CACHE, b.pbs_cache, (1, 2, 3, 4, 5, 6, 7, 8, 9)),
+                           (b._DECODE, b.pbs_decode_problem, (1, 2, 3, 4, 5, 6, 7, 0.25, 9, 10, 11, 12)),
+                           (b._PROMPT, b.pbs_prompt_problem, tuple(range(1, 8)) + (0.5, 9) + tuple(range(10, 18))),
+                           (b._STRIDES, b.pbs_strides, (3, 4))):
+        raw = made(*args)
+        assert len(raw) == ctypes.sizeof(of)
+        x, flat = of.from_buffer_copy(raw), []
+        for name, _ in of._fields_:
+            v = getattr(x, name)
+            flat += [v.token, v.head] if isinstance(v, b.pbs_strides) else [v]
+        assert tuple(flat) == args, of
+    assert struct.calcsize("P") == 8
 
 
 def test_the_binding_refuses_what_the_library_cannot_see():
