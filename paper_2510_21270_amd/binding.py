@@ -641,8 +641,12 @@ class Pipeline:
         self.ws3 = alloc_workspace(p, STAGE_BLOCK_MASK, device)
         self.ws4 = alloc_workspace(p, STAGE_ATTN_FWD, device)
 
-    def run(self, Q, K, V, qidx=None):
+    def run(self, Q, K, V, qidx=None, cache=None, slots=None):
+        """With a `cache` the keys and values also go into its slots [batch, n], for the decode steps behind the prompt."""
         p = self.p
+        if cache is not None:
+            for b in range(p.batch):
+                cache_write(cache, K[b].transpose(0, 1), V[b].transpose(0, 1), slots[b])
         key_scores(p, Q, K, self.scores, self.ws1)
         # the block means of K' that Algorithm 2 starts from come out of the gather (PBS_FLAG_KBAR_IN_WS)
         segment_permute(p, self.scores, K, V, self.kidx, self.Kp, self.Vt, ws=self.ws3)
@@ -651,20 +655,62 @@ class Pipeline:
         attn_fwd(p, Qp, self.Kp, self.Vt, qidx, self.kidx, self.row_cnt, self.col_idx, self.Op, ws=self.ws4)
         return unpermute(p, self.Op, qidx, self.O)
 
-    def capture(self, Q, K, V, qidx=None):
+    def capture(self, Q, K, V, qidx=None, cache=None, slots=None):
         """Record the pipeline into a HIP graph that reads these very tensors (refill them in place, then replay()).
         The library allocates nothing, never synchronises and records no memset nodes, so the calls can be captured
         as they are; short sequences, where the dozen launches cost more than the kernels, gain from it."""
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
-            self.run(Q, K, V, qidx)                        # everything lazily initialised happens outside the capture
+            self.run(Q, K, V, qidx, cache, slots)          # everything lazily initialised happens outside the capture
         torch.cuda.current_stream().wait_stream(side)
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
-            self._graph_out = self.run(Q, K, V, qidx)
+            self._graph_out = self.run(Q, K, V, qidx, cache, slots)
         return self._graph_out
 
     def replay(self):
         self.graph.replay()
         return self._graph_out
+
+
+class DecodeStep:
+    """One step of a batch behind its prompts on preallocated buffers: rotary positions of the new tokens' Q and K (in
+    place), their rows into the cache, attention over the cached keys.  The calls of these names, nothing else."""
+
+    def __init__(self, cache, n_seq, h_q, max_pages, freq, q_len=1, max_len=None, layout="half", magnitude=1.0,
+                 prefix_pages=None, prefix_len=0, scale=0.0):
+        self.cache, self.freq, self.layout, self.magnitude, self.scale = cache, freq, layout, magnitude, scale
+        self.prefix_pages, self.prefix_len = prefix_pages, prefix_len
+        self.max_len = max_pages * cache.page if max_len is None else max_len
+        self.O = torch.empty((n_seq, q_len, h_q, cache.d), dtype=torch.bfloat16, device=cache.K.device)
+        p = _DECODE(n_seq, q_len, h_q, max_pages, self.max_len, prefix_len, PBS_BF16, scale, h_q * cache.d, cache.d,
+                    h_q * cache.d, cache.d)
+        need = load_library().pbs_decode_workspace_bytes(p, cache.c)
+        self.ws = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.K.device)
+
+    def run(self, Q, K, V, positions, slots, page_table, lens):
+        """Q [n_seq, q_len, h_q, d], K and V [n_seq * q_len, h_kv, d] of the new tokens (Q and K are turned in place),
+        positions and slots [n_seq * q_len], page_table [n_seq, max_pages], lens [n_seq] with the new tokens counted."""
+        rows = Q.view(-1, Q.shape[2], Q.shape[3])
+        rope(rows, K, positions, self.freq, self.layout, self.magnitude, Qout=rows, Kout=K)
+        cache_write(self.cache, K, V, slots)
+        return decode_attn(self.cache, Q, page_table, lens, self.max_len, self.prefix_pages, self.prefix_len, self.scale,
+                           self.O, ws=self.ws)
+
+    def capture(self, *args):
+        """Record a step into a HIP graph that reads these very tensors (refill them in place, then replay()).  Q and K are
+        turned by every run, the ones before the recording among them."""
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            self.run(*args)
+        torch.cuda.current_stream().wait_stream(side)
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self.run(*args)
+        return self.O
+
+    def replay(self):
+        self.graph.replay()
+        return self.O
