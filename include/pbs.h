@@ -312,7 +312,7 @@ pbs_status pbs_shader_clock_meter(float *out, int micros, void *stream);
  * These calls see tensors as tokens x heads x features: element (t, h, e) of a tensor lies at t * strides.token +
  * h * strides.head + e, in elements; features are consecutive.  [tokens, heads, d] memory has strides {heads * d, d}, the
  * [1, heads, n, d] memory of the calls above {d, n * d}, and a slice of a fused projection its own.  Base addresses are
- * 16-byte aligned, strides are not negative and whole multiples of 16 bytes; rows of an output do not overlap (all
+ * 16-byte aligned, strides are not negative, below 2^31 and whole multiples of 16 bytes; rows of an output do not overlap (all
  * PBS_ERR_SHAPE otherwise).  d is 64 or 128.  A count of zero tokens or sequences is a call that does nothing.
  * The other conventions above hold: host-validated, nothing allocated, no synchronisation, deterministic.
  */

@@ -14,8 +14,9 @@
 // Ring of four stages; stage p holds K tile p and V tile p - 1 (mod 4), which is what iteration p frees.
 // The softmax of the loop keeps the reference that the first tile sets (any reference gives the same softmax while nothing
 // overflows) and moves it, rescaling O^T and l, when a tile's sum passes 2^40.  What that leaves open (a row whose first
-// tile has no finite logit; values that are not finite, which a hidden key's zero weight would turn into NaN) shows in O^T
-// or l, and such a workgroup goes over its keys again, tile by tile with the running maximum (whole_tile).
+// tile has no finite logit and that ends without a sum; values that are not finite, which a hidden key's zero weight would
+// turn into NaN) shows when the rows are stored, and such a workgroup goes over its keys again, tile by tile with the running
+// maximum (whole_tile), and stores again.
 //
 // F: the keys' and the value rows' factors (of an 8-bit cache whose values lie here as bf16) come along, those of tile t + 3 in
 // iteration t into stage t + 3, and are read four keys at a time where they are needed; a key's multiplies its logit, a
@@ -520,11 +521,10 @@ __device__ __forceinline__ void clear(State<D> &st)
     }
 }
 
-// Keys of tiles 0 .. tiles - 1 (at least one), of which the wave's rows all see those below `all`.  True where the result does not
-// stand: values that are not finite, or a row that sees keys and has no sum.
+// Keys of tiles 0 .. tiles - 1 (at least one), of which the wave's rows all see those below `all`.
 // load_queries brings the rows' queries into q, behind the first tiles' loads.  At the end no load into LDS is left, of either wave.
 template <int D, bool F, class SRC, class LQ>
-__device__ __forceinline__ bool all_tiles(State<D> &st, bf16x8 (&q)[2][D / 16], LQ load_queries, const int (&sees)[2], int all,
+__device__ __forceinline__ void all_tiles(State<D> &st, bf16x8 (&q)[2][D / 16], LQ load_queries, const int (&sees)[2], int all,
                                           int tiles, float c2, const SRC &src, const Offsets<D> &off, Stage<D, F> &sg0, Stage<D, F> &sg1,
                                           Stage<D, F> &sg2, Stage<D, F> &sg3, int wave, int lane)
 {
@@ -586,44 +586,37 @@ __device__ __forceinline__ bool all_tiles(State<D> &st, bf16x8 (&q)[2][D / 16], 
     }
     drain<D>(st, pa, sg0, off);
     meet();
-    float zero = 0.0f;                                     // NaN if a value of O^T is not finite
-    bool bad = false;
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) zero = __builtin_fmaf(st.o[dt][nt][x], 0.0f, zero);
-        const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64);
-        bad = bad || (l == 0.0f && sees[nt] > 0);
-        zero = __builtin_fmaf(l, 0.0f, zero);
-    }
-    return bad || zero != 0.0f;
 }
 
 // Rows of 32 queries out of O^T (lane (n, h), value x of tile dt: feature 32 dt + 8 (x / 4) + 4 h + x % 4 of query n) through
 // LDS, so that a store instruction writes whole rows: make() turns four features into elements E, put(row, piece, value) gets 16
-// bytes of a row.  room: 32 rows of LDS of the wave's own, at most a stage; piece p of row n lies at place p ^ n.
+// bytes of a row.  room: 32 rows of LDS of the wave's own, at most a stage; piece p of row n lies at place p ^ n.  Returns 0, or
+// NaN if a value of the lane's query is not finite.
 template <int D, typename E, class MAKE, class PUT>
-__device__ __forceinline__ void rows_out(const State<D> &st, int nt, unsigned char *room, int lane, MAKE make, PUT put)
+__device__ __forceinline__ float rows_out(const State<D> &st, int nt, unsigned char *room, int lane, MAKE make, PUT put)
 {
     constexpr int kRowB = D * (int)sizeof(E), kPieces = kRowB / 16, kGroup = 4 * (int)sizeof(E);
     typedef E ex4 __attribute__((ext_vector_type(4)));
     const int n = lane & 31, h = lane >> 5;
+    float zero = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const floatx16 &o = st.o[dt][nt];
+            const floatx4 v = {o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) zero = __builtin_fmaf(v[y], 0.0f, zero);
             const int at = (8 * dt + 2 * x + h) * kGroup;
             *reinterpret_cast<ex4 *>(room + n * kRowB + ((at >> 4 ^ (n & (kPieces - 1))) << 4) + (at & 15)) =
-                make(floatx4{o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]});
+                make(v);
         }
-#pragma unroll 2
+#pragma unroll
     for (int y = 0; y < 32 * kPieces / 64; ++y) {
         const int row = (64 * y + lane) / kPieces, piece = lane % kPieces;
         put(row, piece, *reinterpret_cast<const uintx4 *>(room + row * kRowB + ((piece ^ (row & (kPieces - 1))) << 4)));
     }
+    return zero;
 }
 
 }  // namespace prompt

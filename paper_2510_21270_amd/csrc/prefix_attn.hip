@@ -70,7 +70,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const int row = min(row0 + wave * 64 + 32 * nt + n, rows - 1), t = token_of(row);
-            const bf16_t *src = a.Q + (int64_t)t * a.q.token + (int64_t)(kv * a.r + row - t * a.r) * a.q.head + 8 * h;
+            const bf16_t *src = a.Q + row_offset(t, kv * a.r + row - t * a.r, a.q) + 8 * h;
 #pragma unroll
             for (int x = 0; x < D / 16; ++x) q[nt][x] = *reinterpret_cast<const bf16x8 *>(src + 16 * x);
         }
@@ -90,7 +90,8 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         }
     };
     unsigned char *const room = reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1);
-    auto store = [&](const State<D> &st) {
+    auto store = [&](const State<D> &st) {                 // true where the result does not stand
+        bool bad = false;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const int first = row0 + wave * 64 + 32 * nt, row = first + n;
@@ -102,21 +103,21 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             };
             const int64_t parts = (int64_t)part * a.n_seq * a.q_len * a.h_q;
             int t, head;
+            float zero;
             if (single) {
-                rows_out<D, bf16_t>(st, nt, room, lane,
-                                    [&](floatx4 v) { return __builtin_convertvector(l == 0.0f ? floatx4{0} : v * inv, bf16x4); },
+                zero = rows_out<D, bf16_t>(st, nt, room, lane, [&](floatx4 v) { return __builtin_convertvector(v * inv, bf16x4); },
                                     [&](int x, int piece, uintx4 v) {
                                         int ot, oh;
                                         out_of(first + x, ot, oh);
                                         if (first + x < rows)
-                                            *reinterpret_cast<uintx4 *>(a.O + (int64_t)ot * a.o.token + (int64_t)oh * a.o.head + 8 * piece) = v;
+                                            *reinterpret_cast<uintx4 *>(a.O + row_offset(ot, oh, a.o) + 8 * piece) = v;
                                     });
                 if (row < rows && h == 0 && a.lse) {
                     const int64_t out = out_of(row, t, head);
                     a.lse[out] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
                 }
             } else {
-                rows_out<D, float>(st, nt, room, lane, [&](floatx4 v) { return v; },
+                zero = rows_out<D, float>(st, nt, room, lane, [&](floatx4 v) { return v; },
                                    [&](int x, int piece, uintx4 v) {
                                        int ot, oh;
                                        const int64_t out = out_of(first + x, ot, oh);
@@ -128,7 +129,9 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
                     a.part_ml[2 * at + 1] = l;
                 }
             }
+            bad = bad || __builtin_fmaf(l, 0.0f, zero) != 0.0f || l == 0.0f;
         }
+        return bad;
     };
     const auto src = source();
     const Offsets<D> off = offsets<D>(wave, lane, D * 2);
@@ -137,8 +140,8 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     {
         State<D> st;
         clear(st);
-        bad = all_tiles<D, LINE>(st, q, load_queries, sees, count, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane) || missing != 0;
-        store(st);                                         // (nobody waits for the stores)
+        all_tiles<D, LINE>(st, q, load_queries, sees, count, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane);
+        bad = store(st) || missing != 0;                   // (nobody waits for the stores)
     }
     __syncthreads();
     if (__any(bad) && lane == 0) bad_rows = 1;

@@ -63,26 +63,31 @@ __device__ __forceinline__ Place find_place(const Args &a, int b, int lane)
 // row / r for the rows of a workgroup: at least 1 / 2 r off the next whole number
 __device__ __forceinline__ int token_of(const Args &a, int row) { return (int)(((float)row + 0.5f) * a.inv_r); }
 
+// True where the result does not stand: values that are not finite, or a row that sees keys and has no sum.
 template <int D>
-__device__ __forceinline__ void store_rows(const Args &a, const Place &pl, const State<D> &st, int kv, int t0, int rows, int wave,
-                                           int lane, unsigned char *room)
+__device__ __forceinline__ bool store_rows(const Args &a, const Place &pl, const State<D> &st, const int (&sees)[2], int kv, int t0,
+                                           int rows, int wave, int lane, unsigned char *room)
 {
+    bool bad = false;
+    bf16_t *const out = a.O + (int64_t)(pl.q0 + t0) * a.o.token + (int64_t)kv * a.r * a.o.head;
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
         const int row0 = wave * 64 + 32 * nt, row = row0 + (lane & 31);
         const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64), inv = l == 0.0f ? 0.0f : 1.0f / l;
-        rows_out<D, bf16_t>(st, nt, room, lane,
-                            [&](floatx4 v) { return __builtin_convertvector(l == 0.0f ? floatx4{0} : v * inv, bf16x4); },
-                            [&](int x, int piece, uintx4 v) {
-                                const int y = row0 + x, in = token_of(a, y), head = kv * a.r + y - in * a.r;
-                                if (y < rows)
-                                    *reinterpret_cast<uintx4 *>(a.O + (int64_t)(pl.q0 + t0 + in) * a.o.token + (int64_t)head * a.o.head + 8 * piece) = v;
-                            });
+        // (no sum: O^T is zero as well)
+        const float zero = rows_out<D, bf16_t>(st, nt, room, lane, [&](floatx4 v) { return __builtin_convertvector(v * inv, bf16x4); },
+                                               [&](int x, int piece, uintx4 v) {
+                                                   const int y = row0 + x, in = token_of(a, y);
+                                                   if (y < rows)
+                                                       *reinterpret_cast<uintx4 *>(out + row_offset(in, y - in * a.r, a.o) + 8 * piece) = v;
+                                               });
+        bad = bad || __builtin_fmaf(l, 0.0f, zero) != 0.0f || (l == 0.0f && sees[nt] > 0);
         if (a.lse && lane < 32 && row < rows) {
             const int in = token_of(a, row), head = kv * a.r + row - in * a.r;
             a.lse[(int64_t)(pl.q0 + t0 + in) * a.h_q + head] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
         }
     }
+    return bad;
 }
 
 template <int D>
@@ -102,12 +107,13 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     int sees[2];
     State<D> st;
     clear(st);
+    const bf16_t *const first = a.Q + (int64_t)(pl.q0 + t0) * a.q.token + (int64_t)kv * a.r * a.q.head;
     auto load_queries = [&]() {
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const int row = wave * 64 + 32 * nt + n, rc = min(row, rows - 1);
-            const int in = token_of(a, rc), head = kv * a.r + rc - in * a.r;
-            const bf16_t *src = a.Q + (int64_t)(pl.q0 + t0 + in) * a.q.token + (int64_t)head * a.q.head + 8 * h;
+            const int in = token_of(a, rc);
+            const bf16_t *src = first + row_offset(in, rc - in * a.r, a.q) + 8 * h;
 #pragma unroll
             for (int x = 0; x < D / 16; ++x) q[nt][x] = *reinterpret_cast<const bf16x8 *>(src + 16 * x);
         }
@@ -130,12 +136,11 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     src.tile_bytes = KS * step_bytes;
     const Offsets<D> off = offsets<D>(wave, lane, (uint32_t)step_bytes);
     if (threadIdx.x == 0) bad_rows = 0;
-    bool bad = false;
     if (tiles > 0) {
         const int all = __builtin_amdgcn_readfirstlane(sees[0]);               // the wave's first row sees the fewest keys
-        bad = all_tiles<D, false>(st, q, load_queries, sees, all, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane);
+        all_tiles<D, false>(st, q, load_queries, sees, all, tiles, a.c2, src, off, sg0, sg1, sg2, sg3, wave, lane);
     }
-    store_rows<D>(a, pl, st, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));   // (nobody waits for the stores)
+    const bool bad = store_rows<D>(a, pl, st, sees, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));   // (nobody waits for the stores)
     __syncthreads();
     if (__any(bad) && lane == 0) bad_rows = 1;
     __syncthreads();
@@ -149,7 +154,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             whole_tile<D>(st, sg0, off, q, sees, t * KS, 3, a.c2, h);
         }
         __syncthreads();
-        store_rows<D>(a, pl, st, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));
+        const bool bad = store_rows<D>(a, pl, st, sees, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));
     }
 }
 

@@ -6,11 +6,18 @@ namespace pbs {
 
 inline bool good_strides(const pbs_strides &s, int es)
 {
-    return s.token >= 0 && s.head >= 0 && s.token * es % 16 == 0 && s.head * es % 16 == 0 && s.token < (1ll << 40) &&
-           s.head < (1ll << 40);
+    return s.token >= 0 && s.head >= 0 && s.token * es % 16 == 0 && s.head * es % 16 == 0 && s.token < (1ll << 31) &&
+           s.head < (1ll << 31);
 }
 
 inline bool good_input(const void *x, const pbs_strides &s, int es) { return aligned16(x) && good_strides(s, es); }
+
+// Element offset of a row of which token and head are small and not negative: strides have 31 bits, so that two multiply-adds of
+// 32 bits do (a product of 64 bits each takes eight instructions of a quarter of the rate).
+__host__ __device__ __forceinline__ uint64_t row_offset(uint32_t token, uint32_t head, const pbs_strides &s)
+{
+    return (uint64_t)token * (uint32_t)s.token + (uint64_t)head * (uint32_t)s.head;
+}
 
 // rows of an output do not overlap: the finer of the two steps covers a row, the coarser one all rows of the finer
 inline bool good_output(const void *x, const pbs_strides &s, long long tokens, long long heads, int d, int es)
