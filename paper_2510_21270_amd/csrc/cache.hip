@@ -170,7 +170,7 @@ inline pbs_status cache_args(const pbs_cache *c, int32_t dtype, int32_t tokens, 
     if (st != PBS_OK) return st;
     if (dtype != PBS_F32 && dtype != PBS_BF16) return PBS_ERR_UNSUPPORTED;
     if (tokens < 0) return PBS_ERR_SHAPE;
-    if ((long long)tokens * c->h_kv > 0x7fffffffLL) return PBS_ERR_UNSUPPORTED;
+    if ((long long)tokens * c->h_kv > 0x7fffff00LL) return PBS_ERR_UNSUPPORTED;             // the last workgroup's rows are ints too
     if (tokens > 0 && !slots) return PBS_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(slots) & 3u) != 0) return PBS_ERR_SHAPE;
     a.rows = tokens * c->h_kv;

@@ -30,7 +30,8 @@ struct DecodeArgs {
     float *line_kf, *line_vf;
 };
 
-// The prefix against more rows than a wave of decode_attn.hip takes (prefix_attn.hip).  single: its one part is the result.
-pbs_status launch_prefix(const DecodeArgs &a, int dtype, int d, bool single, hipStream_t s);
+// The prefix against more rows than a wave of decode_attn.hip takes (prefix_attn.hip).  Always into the workspace: it may read
+// its queries twice, and O may be Q.
+pbs_status launch_prefix(const DecodeArgs &a, int dtype, int d, hipStream_t s);
 
 }  // namespace pbs

@@ -630,7 +630,7 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     if (a.shares > most) a.shares = (int)most;
     plan.grid = ((plan.whole ? units : a.max_len > 0 ? a.shares : 0) + kDecWaves - 1) / kDecWaves;
     a.shares = (int)(plan.whole ? 0 : plan.grid * kDecWaves);
-    plan.join = !plan.whole && !(plan.grid == 0 && a.p_parts == 1);
+    plan.join = !plan.whole && !(plan.grid == 0 && a.p_parts == 1 && plan.p_nt > 0);
     const size_t all = plan.join ? (size_t)a.n_seq * a.q_len * a.h_q * (size_t)a.p_parts : 0;
     const size_t slots = plan.join && plan.grid ? (size_t)(units + a.shares) * a.slot_rows : 0;
     size_t at = 0;
@@ -664,7 +664,7 @@ pbs_status launch_decode(const DecodePlan &plan, hipStream_t s)
     const DecodeArgs &a = plan.a;
     pbs_status st = PBS_OK;
     if (a.p_parts > 0 && plan.p_nt == 0) {
-        st = launch_prefix(a, DTYPE, D, !plan.join, s);
+        st = launch_prefix(a, DTYPE, D, s);
     } else if (a.p_parts > 0) {
         auto kernel = plan.p_nt == 1 ? decode_prefix_kernel<DTYPE, D, 1> : decode_prefix_kernel<DTYPE, D, 2>;
         st = launch(kernel, dim3(a.h_kv, a.p_row_tiles, a.p_parts), dim3(kDecThreads), 0, s, a, !plan.join);

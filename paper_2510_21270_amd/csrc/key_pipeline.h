@@ -597,6 +597,7 @@ __device__ __forceinline__ float rows_out(const State<D> &st, int nt, unsigned c
 {
     constexpr int kRowB = D * (int)sizeof(E), kPieces = kRowB / 16, kGroup = 4 * (int)sizeof(E);
     typedef E ex4 __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(E) == 4) asm volatile("" : "+v"(lane));  // addresses are formed here, not ahead of the loop
     const int n = lane & 31, h = lane >> 5;
     float zero = 0.0f;
 #pragma unroll

@@ -43,7 +43,7 @@ struct Pages {
 
 // LINE: the keys lie in order as bf16 with factors beside them.  HALVES: in pages of 16.
 template <int D, bool LINE, bool HALVES>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void prefix_kernel(DecodeArgs a, bool single)
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void prefix_kernel(DecodeArgs a)
 {
     __shared__ Stage<D, LINE> sg0, sg1, sg2, sg3;
     __shared__ int bad_rows;
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     }
     // row / r: the workgroup's first row by a division, its 128 rows by 1 / r, at least 1 / 2 r off the next whole number
     const int t0 = row0 / a.r, rest = row0 - t0 * a.r;
-    const float inv_r = 1.0f / (float)a.r;
+    const float inv_r = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, 1.0f / (float)a.r)));
     auto token_of = [&](int row) { return t0 + (int)(((float)(row - row0 + rest) + 0.5f) * inv_r); };
     bf16x8 q[2][D / 16];
     const int sees[2] = {count, count};
@@ -92,42 +92,26 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     unsigned char *const room = reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1);
     auto store = [&](const State<D> &st) {                 // true where the result does not stand
         bool bad = false;
+        int lane_here = lane;
+        asm volatile("" : "+v"(lane_here));                // as in rows_out
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-            const int first = row0 + wave * 64 + 32 * nt, row = first + n;
-            const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64), inv = l == 0.0f ? 0.0f : 1.0f / l;
-            auto out_of = [&](int y, int &t, int &head) {
-                t = token_of(y);
-                head = kv * a.r + y - t * a.r;
-                return (int64_t)t * a.h_q + head;
+            const int first = row0 + wave * 64 + 32 * nt, row = first + (lane_here & 31);
+            const float l = st.l[nt] + __shfl_xor(st.l[nt], 32, 64);
+            auto out_of = [&](int y) {
+                const int t = token_of(y);
+                return (int64_t)t * a.h_q + kv * a.r + y - t * a.r;
             };
             const int64_t parts = (int64_t)part * a.n_seq * a.q_len * a.h_q;
-            int t, head;
-            float zero;
-            if (single) {
-                zero = rows_out<D, bf16_t>(st, nt, room, lane, [&](floatx4 v) { return __builtin_convertvector(v * inv, bf16x4); },
-                                    [&](int x, int piece, uintx4 v) {
-                                        int ot, oh;
-                                        out_of(first + x, ot, oh);
-                                        if (first + x < rows)
-                                            *reinterpret_cast<uintx4 *>(a.O + row_offset(ot, oh, a.o) + 8 * piece) = v;
-                                    });
-                if (row < rows && h == 0 && a.lse) {
-                    const int64_t out = out_of(row, t, head);
-                    a.lse[out] = l == 0.0f ? -INFINITY : (st.m[nt] + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-                }
-            } else {
-                zero = rows_out<D, float>(st, nt, room, lane, [&](floatx4 v) { return v; },
-                                   [&](int x, int piece, uintx4 v) {
-                                       int ot, oh;
-                                       const int64_t out = out_of(first + x, ot, oh);
-                                       if (first + x < rows) *reinterpret_cast<uintx4 *>(a.part_o + (parts + out) * D + 4 * piece) = v;
-                                   });
-                if (row < rows && h == 0) {
-                    const int64_t at = parts + out_of(row, t, head);
-                    a.part_ml[2 * at] = st.m[nt];
-                    a.part_ml[2 * at + 1] = l;
-                }
+            const float zero = rows_out<D, float>(st, nt, room, lane, [&](floatx4 v) { return v; },
+                                                  [&](int x, int piece, uintx4 v) {
+                                                      if (first + x < rows)
+                                                          *reinterpret_cast<uintx4 *>(a.part_o + (parts + out_of(first + x)) * D + 4 * piece) = v;
+                                                  });
+            if (row < rows && h == 0) {
+                const int64_t at = parts + out_of(row);
+                a.part_ml[2 * at] = st.m[nt];
+                a.part_ml[2 * at + 1] = l;
             }
             bad = bad || __builtin_fmaf(l, 0.0f, zero) != 0.0f || l == 0.0f;
         }
@@ -187,20 +171,20 @@ __global__ __launch_bounds__(256) void line_kernel(DecodeArgs a)
 
 }  // namespace prompt
 
-pbs_status launch_prefix(const DecodeArgs &a, int dtype, int d, bool single, hipStream_t s)
+pbs_status launch_prefix(const DecodeArgs &a, int dtype, int d, hipStream_t s)
 {
     using namespace prompt;
     const dim3 grid(a.h_kv, a.p_row_tiles, a.p_parts), block(128);
     if (dtype == PBS_BF16) {
         auto kernel = d == 128 ? (a.page_log == 4 ? prefix_kernel<128, false, true> : prefix_kernel<128, false, false>)
                                : (a.page_log == 4 ? prefix_kernel<64, false, true> : prefix_kernel<64, false, false>);
-        return launch(kernel, grid, block, 0, s, a, single);
+        return launch(kernel, grid, block, 0, s, a);
     }
     auto line = d == 128 ? (dtype == PBS_E4M3 ? line_kernel<PBS_E4M3, 128> : line_kernel<PBS_I8, 128>)
                          : (dtype == PBS_E4M3 ? line_kernel<PBS_E4M3, 64> : line_kernel<PBS_I8, 64>);
     const pbs_status st = launch(line, dim3((unsigned)(((int64_t)a.p_room * (d / 8) + 255) / 256), a.h_kv), dim3(256), 0, s, a);
     if (st != PBS_OK) return st;
-    return launch(d == 128 ? prefix_kernel<128, true, false> : prefix_kernel<64, true, false>, grid, block, 0, s, a, single);
+    return launch(d == 128 ? prefix_kernel<128, true, false> : prefix_kernel<64, true, false>, grid, block, 0, s, a);
 }
 
 }  // namespace pbs

@@ -312,6 +312,15 @@ def test_decode_prefix_of_a_large_batch_with_odd_pages_and_values(held):
         assert torch.isnan(got[:, :, 8:]).all()
 
 
+def test_decode_prefix_of_a_large_batch_in_place_with_values_that_are_not_finite():
+    # the prefix alone, in one part: rows that are formed again read their queries again, and O is Q
+    s = Setup(33, 1, 40, 1, 64, "bf16", 16, [0], 90)
+    s.cache.V[int(s.prefix_pages[1]), 0, 4, 5] = math.inf
+    want = s.call()
+    Q = s.Q.cuda()
+    assert torch.equal(s.call(Q=Q, O=Q, max_len=0), want) and bool((want[..., 5] == math.inf).all())
+
+
 def test_decode_prefix_of_a_large_batch_logits_that_grow():
     s = Setup(32, 1, 40, 1, 128, "i8", 32, [5], 900)
     s.Q *= 30                                              # hundreds of nats between keys

@@ -87,7 +87,8 @@ def test_the_loop_moves_nothing_between_register_files(kernels):
         loop = [b for b in blocks if sum("mfma" in l for l in b) == per and sum("v_exp_f32" in l for l in b) == 32]
         assert len(loop) == 4, (name, len(loop))
         for b in loop:
-            assert sum("accvgpr" in l for l in b) <= (2 if "prompt_kernel" in name else 10), name
+            # a prefix with factors beside its values keeps nine load offsets and a few more there, each read once to a tile
+            assert sum("accvgpr" in l for l in b) <= (2 if "prompt_kernel" in name else 12), name
             assert not any("scratch" in l for l in b), name
             # a prefix's tiles have an address each, or factors
             most = (210 if per == 32 else 170) + (0 if "prompt_kernel" in name else 60)
