@@ -406,16 +406,17 @@ pbs_status pbs_cache_read(const pbs_cache *c, int32_t dtype, int32_t tokens, con
  *   page_table [n_seq, max_pages] int32: the pages of a sequence's own keys in order; entries behind its length are
  *            not looked at.  A listed page outside [0, pages) counts as keys that nobody sees.
  *   lens     [n_seq] int32, device memory: own keys; negative counts as 0, more than min(max_len, max_pages * page) as that.
- *   max_len  an upper bound of lens that the host knows: it decides how the work is cut, not what comes out.
- *   prefix_pages [ceil(prefix_len / page)] int32, device memory; NULL when prefix_len is 0.  The prefix is read once
- *            for the whole batch, not once per sequence.
+ *   max_len  an upper bound of lens that the host knows; how the work is cut follows lens themselves, but a small bound
+ *            needs fewer workgroups and, up to 128, no workspace.
+ *   prefix_pages [ceil(prefix_len / page)] int32, device memory; NULL when prefix_len is 0.  The prefix is read for 16 to
+ *            128 rows (query, head of its group) of the whole batch at a time, not once per sequence.
  *   lse      [n_seq * q_len, h_q] float32 or NULL: log-sum-exp of the logits that each query sees.
  *   ws       pbs_decode_workspace_bytes(p, c) bytes, 256-byte aligned (0: may be NULL); need not be initialised, means
  *            nothing afterwards.  Calls that may overlap in time need one each.
  * Probabilities enter the second product in bf16, everything else is fp32.
  * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE (max_len or prefix_len negative, misaligned, a scale that is negative or not
- * finite), PBS_ERR_UNSUPPORTED (q_len > 16, n_seq * q_len * h_q or n_seq * max_pages > 2^31 - 1 or a grid that is too large,
- * dtype), PBS_ERR_WORKSPACE, PBS_ERR_HIP.
+ * finite), PBS_ERR_UNSUPPORTED (q_len > 16, n_seq > 65535, n_seq * q_len * h_q or n_seq * max_pages > 2^31 - 1,
+ * max_len > 2^27, prefix_len > 2^25, a grid that is too large, dtype), PBS_ERR_WORKSPACE, PBS_ERR_HIP.
  */
 typedef struct {
     int32_t n_seq, q_len, h_q;

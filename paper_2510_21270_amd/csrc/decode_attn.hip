@@ -563,12 +563,33 @@ __global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, 
     store_output(a, token, head, 4 * x, out, m, l);
 }
 
-// Keys of a part of the prefix: the longest of 128, 256, ... 4096 with which the call has `wanted` workgroups.
-inline int part_keys(int64_t units, int64_t keys, int64_t wanted)
+// Keys of a part of the prefix, for decode_prefix_kernel: one workgroup to a compute unit, or as few rounds of them as parts of
+// kMostChunk keys allow, and no more than 64 parts for fewer rounds' sake: the join reads them all.  Measured, whole call, d = 128,
+// 8 kv heads: 128 / 256 / 512 workgroups take 33 / 28 / 33 us for 64 rows of 8000 keys in bf16 and 76 / 50 / 56 us for 32000 in
+// e4m3; 2 kv heads, 16 rows, 32000 keys: 64 parts 25 us, 128 parts 29 us.
+inline int part_keys(int64_t units, int64_t keys)
 {
-    int chunk = kMostChunk;
-    while (chunk > 128 && units * ((keys + chunk - 1) / chunk) < wanted) chunk >>= 1;
-    return chunk;
+    if (units < 1 || keys < 1) return kMostChunk;
+    const int64_t least = (keys + kMostChunk - 1) / kMostChunk, rounds = (least * units + 255) / 256;
+    int64_t parts = rounds * 256 / units;
+    if (parts > 64) parts = 64;
+    if (parts < least) parts = least;
+    const int64_t chunk = ((keys + parts - 1) / parts + 127) / 128 * 128;
+    return chunk > kMostChunk ? kMostChunk : chunk < 128 ? 128 : (int)chunk;
+}
+
+// Whether decode_prefix_kernel, 16 or 32 rows to a workgroup, reads the prefix, or, from more rows on, the kernel of
+// prefix_attn.hip, 128 rows to a workgroup.  The latter multiplies faster but starts and ends slower, and it wants 8-bit values
+// written out as bf16, which costs as much as four passes of the former over them.  Measured, whole call, us, this kernel / that:
+// bf16, 8 kv heads, 8000 keys: 64 rows 28 / 34, 128 rows 35 / 37, 160 rows 39 / 36, 256 rows 49 / 40; 2000 keys, 256 rows 28 / 35;
+// 32000 keys, 96 rows 62 / 48.  e4m3: 8000 keys, 128 rows 34 / 49, 256 rows 50 / 51; 32000 keys, 128 rows 77 / 84, 256 rows
+// 139 / 100.
+inline int prefix_tiles(int64_t rows, int h_kv, int64_t keys, int dtype)
+{
+    if (rows <= 16) return 1;
+    const int64_t tiles = (rows + 31) / 32, work = tiles * h_kv * keys;
+    if (rows <= 32) return 2;
+    return dtype == PBS_BF16 ? (work <= 1 << 18 ? 2 : 0) : (tiles <= 4 || work <= 1 << 19 ? 2 : 0);
 }
 
 struct DecodePlan {
@@ -592,7 +613,7 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     if (p->dtype != PBS_BF16 || p->q_len > kMostQueries) return PBS_ERR_UNSUPPORTED;
     if ((long long)p->n_seq * p->q_len * p->h_q > 0x7fffffffLL || (long long)p->n_seq * p->max_pages > 0x7fffffffLL)
         return PBS_ERR_UNSUPPORTED;
-    if (p->max_len > 1 << 27 || p->prefix_len > 1 << 27) return PBS_ERR_UNSUPPORTED;         // sums of tiles are ints
+    if (p->max_len > 1 << 27 || p->prefix_len > 1 << 25) return PBS_ERR_UNSUPPORTED;         // sums of tiles and rows of parts are ints
     DecodeArgs &a = plan.a;
     a.n_seq = p->n_seq; a.q_len = p->q_len; a.h_q = p->h_q; a.h_kv = c->h_kv; a.r = p->h_q / c->h_kv;
     a.page_log = log2_of(c->page); a.pages = c->pages; a.max_pages = p->max_pages;
@@ -603,14 +624,14 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     a.q = p->q; a.o = p->o;
     const int64_t rows = (int64_t)a.q_len * a.r, p_rows = rows * a.n_seq;
     plan.nt = rows <= 16 ? 1 : 2;
-    plan.p_nt = p_rows <= 16 ? 1 : p_rows <= 32 ? 2 : 0;   // 0: the kernel for many rows
+    plan.p_nt = prefix_tiles(p_rows, c->h_kv, a.prefix_len, c->dtype);     // 0: the kernel for many rows
     a.row_tiles = (int)((rows + 16 * plan.nt - 1) / (16 * plan.nt));
     a.units = a.h_kv * a.row_tiles;
     a.slot_rows = (int)(rows < 16 * plan.nt ? rows : 16 * plan.nt);
     const int64_t p_tile = plan.p_nt ? 16 * plan.p_nt : kPrefixRows;
     a.p_row_tiles = (int)((p_rows + p_tile - 1) / p_tile);
     if (plan.p_nt) {
-        a.p_chunk = part_keys((int64_t)a.h_kv * a.p_row_tiles, a.prefix_len, 128);
+        a.p_chunk = part_keys((int64_t)a.h_kv * a.p_row_tiles, a.prefix_len);
     } else {
         // two workgroups to a compute unit, whole turns of the loop, pages of a part in a wave's lanes
         const int64_t units = (int64_t)a.h_kv * a.p_row_tiles, parts = (512 + units - 1) / units;

@@ -321,6 +321,58 @@ def test_decode_prefix_of_a_large_batch_in_place_with_values_that_are_not_finite
     assert torch.equal(s.call(Q=Q, O=Q, max_len=0), want) and bool((want[..., 5] == math.inf).all())
 
 
+# rows times keys large enough for the kernel with 128 rows to a workgroup; the last part of the prefix has 65, 1, 127, 5 keys
+@pytest.mark.parametrize("n,h_q,h_kv,d,page,prefix", [(8, 16, 1, 64, 16, 4161), (9, 16, 1, 128, 16, 4097), (7, 32, 2, 128, 64, 2431),
+                                                      (5, 32, 1, 64, 256, 3333)])
+def test_decode_prefix_of_thousands_of_rows(n, h_q, h_kv, d, page, prefix):
+    s = Setup(34, 16, h_q, h_kv, d, "bf16", page, [(5 * i) % 40 for i in range(n)], prefix)
+    O, lse = s.call(want_lse=True)
+    s.check(O, lse)
+    assert torch.equal(O, s.call())
+
+
+@pytest.mark.parametrize("held,n,h_q,h_kv,d,page,prefix", [("e4m3", 9, 32, 1, 64, 16, 3700), ("i8", 10, 32, 2, 128, 32, 3329),
+                                                           ("e4m3", 10, 32, 2, 128, 128, 3383)])
+def test_decode_prefix_of_thousands_of_rows_8_bit(held, n, h_q, h_kv, d, page, prefix):
+    s = Setup(35, 16, h_q, h_kv, d, held, page, [(5 * i) % 40 for i in range(n)], prefix)
+    O, lse = s.call(want_lse=True)
+    s.check(O, lse)
+    assert torch.equal(O, s.call())
+
+
+@pytest.mark.parametrize("held", ["bf16", "e4m3"])
+def test_decode_prefix_of_thousands_of_rows_with_odd_pages_and_values(held):
+    n, prefix = (9, 4300) if held == "bf16" else (18, 4300)
+    s = Setup(36, 16, 16, 1, 128, held, 16, [3] * n, prefix)
+    s.Q *= 8                                               # logits that grow
+    s.prefix_pages[4], s.prefix_pages[11], s.prefix_pages[-1] = -1, 77777, -1
+
+    def hidden(i, j):
+        return ((j >= 64) & (j < 80)) | ((j >= 176) & (j < 192)) | ((j >= 4288) & (j < 4300))
+
+    O, lse = s.call(want_lse=True)
+    s.check(O, lse, hidden)
+    page = int(s.prefix_pages[2])
+    if held == "bf16":
+        s.cache.V[page, 0, 3, 9] = math.inf
+        got = s.call().float().cpu()
+        assert not torch.isfinite(got[..., 9]).any()       # its probability may be 0: NaN
+        got[..., 9] = 0
+        assert torch.isfinite(got).all()
+    else:
+        s.cache.v_scale[page, 0, 3] = math.nan
+        assert torch.isnan(s.call()).all()
+
+
+def test_decode_prefix_of_thousands_of_rows_in_place_with_values_that_are_not_finite():
+    # the prefix alone, in one part: rows that are formed again read their queries again, and O is Q
+    s = Setup(37, 16, 4, 4, 64, "bf16", 16, [0] * 1024, 200)
+    s.cache.V[int(s.prefix_pages[1]), :, 4, 5] = math.inf
+    want = s.call()
+    Q = s.Q.cuda()
+    assert torch.equal(s.call(Q=Q, O=Q, max_len=0), want) and bool((want[..., 5] == math.inf).all())
+
+
 def test_decode_prefix_of_a_large_batch_logits_that_grow():
     s = Setup(32, 1, 40, 1, 128, "i8", 32, [5], 900)
     s.Q *= 30                                              # hundreds of nats between keys

@@ -160,11 +160,12 @@ def test_decode_refusals(lib):
     for name in ("Q", "table", "lens", "O"):
         assert call(**{name: None}) == 1, name
     assert call(_decode(prefix_len=5), prefix=None) == 1
-    assert call(_decode(n_seq=0), Q=None) == 0
+    assert call(_decode(n_seq=0), Q=None) == 0 and call(_decode(n_seq=0, prefix_len=100), Q=None) == 0
     for kw in (dict(n_seq=-1), dict(q_len=0), dict(h_q=0), dict(h_q=3), dict(max_pages=-1), dict(max_len=-1), dict(prefix_len=-1),
                dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf)):
         assert call(_decode(**kw)) == 2, kw
-    for kw in (dict(q_len=17), dict(dtype=0), dict(n_seq=70000), dict(n_seq=60000, max_pages=60000), dict(prefix_len=2 ** 31 - 1)):
+    for kw in (dict(q_len=17), dict(dtype=0), dict(n_seq=70000), dict(n_seq=60000, max_pages=60000), dict(prefix_len=2 ** 31 - 1),
+               dict(prefix_len=2 ** 25 + 1), dict(max_len=2 ** 27 + 1)):
         assert call(_decode(**kw)) == 3, kw
     for kw, st in BAD_CACHES:
         assert call(c=_cache(**kw)) == st, kw
