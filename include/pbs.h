@@ -407,7 +407,7 @@ pbs_status pbs_cache_read(const pbs_cache *c, int32_t dtype, int32_t tokens, con
  *            not looked at.  A listed page outside [0, pages) counts as keys that nobody sees.
  *   lens     [n_seq] int32, device memory: own keys; negative counts as 0, more than min(max_len, max_pages * page) as that.
  *   max_len  an upper bound of lens that the host knows; how the work is cut follows lens themselves, but a small bound
- *            needs fewer workgroups and, up to 128, no workspace.
+ *            needs fewer workgroups and no workspace (without a prefix: up to 128, with many sequences up to 512).
  *   prefix_pages [ceil(prefix_len / page)] int32, device memory; NULL when prefix_len is 0.  The prefix is read for 16 to
  *            128 rows (query, head of its group) of the whole batch at a time, not once per sequence.
  *   lse      [n_seq * q_len, h_q] float32 or NULL: log-sum-exp of the logits that each query sees.

@@ -26,9 +26,9 @@ constexpr int kDecThreads = 64 * kDecWaves;
 constexpr int kTileKeys = 32;
 constexpr int kMostChunk = 4096;                           // keys of a part of the prefix
 constexpr int kHeldTiles = 32;                             // tiles whose pages (two each) a wave's lanes hold
-constexpr int kWholeKeys = 128;                            // lengths up to which a unit has a wave to itself
-constexpr int kUnitCost = 2;                               // tiles
+constexpr int kUnitCost = 2;                               // tiles, for 16 rows
 constexpr int kMostQueries = 16;
+constexpr int kFewPieces = 8;                              // of a row that one wave joins
 
 // own keys of sequence i
 __device__ __forceinline__ int own_len(const DecodeArgs &a, int i)
@@ -308,8 +308,11 @@ __device__ __forceinline__ void store_output(const DecodeArgs &a, int token, int
 }
 
 __device__ __forceinline__ int tiles_of(const DecodeArgs &a, int i) { return ceil_div(own_len(a, i), kTileKeys); }
-// what a unit of n tiles counts as: its start and its end cost a wave about as much as kUnitCost tiles
-__device__ __forceinline__ int cost_of(int n) { return n > 0 ? n + kUnitCost : 0; }
+// What a unit of n tiles counts as: its start and its end cost a wave about as much as kUnitCost tiles.  Measured with 0 / 1 / 2 / 4 / 8:
+// 64 sequences of 7 .. 16000 keys in e4m3, 8 kv heads, 77 / 63 / 62 / 63 / 65 us; 100 of 10 .. 600 21.5 / 21.2 / 21.1 / 21.9 / 24.1;
+// two tiles of rows to a wave, 16 sequences of 10 .. 5000: 30.5 / 29.2 / 28.9 / 25.7 / 25.7.
+template <int NT>
+__device__ __forceinline__ int cost_of(int n) { return n > 0 ? n + kUnitCost * NT : 0; }
 
 // Sum over the workgroup, and in `before` the sum over the threads in front of this one.
 __device__ __forceinline__ int scan_group(int v, int &before, int *sums)
@@ -389,13 +392,13 @@ __global__ __launch_bounds__(kDecThreads, NT == 1 ? 2 : 1) void decode_own_kerne
     int before;
     for (int base = 0; base < a.n_seq; base += kDecThreads) {
         const int x = base + threadIdx.x;
-        total += scan_group(x < a.n_seq ? cost_of(tiles_of(a, x)) : 0, before, sums);
+        total += scan_group(x < a.n_seq ? cost_of<NT>(tiles_of(a, x)) : 0, before, sums);
     }
     const int64_t share = max((total * a.units + a.shares - 1) / a.shares, (int64_t)1), all = total * a.units;
     // the sequence that each wave's share begins in, and the cost of those in front of it
     int64_t front = 0;
     for (int base = 0; base < a.n_seq; base += kDecThreads) {
-        const int x = base + threadIdx.x, n = x < a.n_seq ? cost_of(tiles_of(a, x)) : 0;
+        const int x = base + threadIdx.x, n = x < a.n_seq ? cost_of<NT>(tiles_of(a, x)) : 0;
         const int sum = scan_group(n, before, sums);
         const int64_t mine = (front + before) * a.units;
 #pragma unroll
@@ -413,12 +416,12 @@ __global__ __launch_bounds__(kDecThreads, NT == 1 ? 2 : 1) void decode_own_kerne
     const int64_t stop = min(at + share, all);
     if (at >= stop) return;
     int i = __builtin_amdgcn_readfirstlane(found[wave]);
-    int len = __builtin_amdgcn_readfirstlane(own_len(a, i)), n = ceil_div(len, kTileKeys), cost = cost_of(n);
+    int len = __builtin_amdgcn_readfirstlane(own_len(a, i)), n = ceil_div(len, kTileKeys), cost = cost_of<NT>(n);
     const int64_t inside = at - found_front[wave];         // of the sequence's units, in tiles
     int k = __builtin_amdgcn_readfirstlane((int)(inside / cost)), off = __builtin_amdgcn_readfirstlane((int)(inside - (int64_t)k * cost));
     while (true) {
         const int take = (int)min((int64_t)(cost - off), stop - at);
-        const int first = max(off - kUnitCost, 0), last = off + take - kUnitCost;             // tiles
+        const int first = max(off - kUnitCost * NT, 0), last = off + take - kUnitCost * NT;             // tiles
         const int64_t unit = (int64_t)i * a.units + k, slot = w + unit;       // one of the two moves on with every piece
         if (last > first) {
             if (first == 0 && (threadIdx.x & 63) == 0)
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(kDecThreads, NT == 1 ? 2 : 1) void decode_own_kerne
             } while (len == 0);                            // tiles are left, so there is a sequence with some
             len = __builtin_amdgcn_readfirstlane(len);
             n = ceil_div(len, kTileKeys);
-            cost = cost_of(n);
+            cost = cost_of<NT>(n);
         }
     }
 }
@@ -507,60 +510,123 @@ __global__ __launch_bounds__(kDecThreads, NT == 1 ? 2 : 1) void decode_prefix_ke
     }
 }
 
-// One workgroup per row, groups of D / 4 threads: every group takes every eighth (d = 64: sixteenth) of the prefix's parts and the
-// unit's pieces.  rows_of_unit: 16 NT.
-template <int D>
-__global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, int rows_of_unit)
+// What lies of a row in the workspace: the prefix's parts, the pieces of its unit's own keys.
+struct JoinRow {
+    int64_t row, all_rows, slot;
+    int token, head, parts, all, in_unit;
+    bool done;                                             // stored where it was computed
+};
+__device__ __forceinline__ JoinRow join_row(const DecodeArgs &a, int64_t row, int rows_of_unit)
 {
-    constexpr int L = D / 4, G = kDecThreads / L;
-    __shared__ __align__(16) float so[G][D];
-    __shared__ float sl[G], sm[kDecWaves];
-    const int64_t row = blockIdx.x, all_rows = (int64_t)a.n_seq * a.q_len * a.h_q;
-    const int token = (int)(row / a.h_q), head = (int)(row - (int64_t)token * a.h_q);
-    const int i = token / a.q_len, h = head / a.r, in_seq = (token - i * a.q_len) * a.r + head - h * a.r;
+    JoinRow j;
+    j.row = row;
+    j.all_rows = (int64_t)a.n_seq * a.q_len * a.h_q;
+    j.token = (int)(row / a.h_q);
+    j.head = (int)(row - (int64_t)j.token * a.h_q);
+    const int i = j.token / a.q_len, h = j.head / a.r, in_seq = (j.token - i * a.q_len) * a.r + j.head - h * a.r;
     const int tile = in_seq / rows_of_unit;
     const int64_t unit = (int64_t)i * a.units + tile * a.h_kv + h;
     int2 own = make_int2(0, 0);
     if (a.shares > 0 && own_len(a, i) > 0) own = a.pieces[unit];
-    if (a.p_parts == 0 && own.y == 1) return;              // stored where it was computed
-    const int64_t slot = own.x + unit;
-    const int all = a.p_parts + own.y;
-    auto place = [&](int p) {
-        return p < a.p_parts ? p * all_rows + row : (slot + p - a.p_parts) * a.slot_rows + in_seq - tile * rows_of_unit;
-    };
-    float m = -INFINITY;
-    for (int p = threadIdx.x; p < all; p += kDecThreads) m = fmaxf(m, (p < a.p_parts ? a.part_ml : a.piece_ml)[2 * place(p)]);
-    m = wave_max(m);
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-    const int group = threadIdx.x / L, x = threadIdx.x % L;
-    float l = 0.0f;
-    floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    j.slot = own.x + unit;
+    j.parts = a.p_parts;
+    j.all = a.p_parts + own.y;
+    j.in_unit = in_seq - tile * rows_of_unit;
+    j.done = a.p_parts == 0 && own.y == 1;
+    return j;
+}
+__device__ __forceinline__ int64_t place_of(const DecodeArgs &a, const JoinRow &j, int p)
+{
+    return p < j.parts ? p * j.all_rows + j.row : (j.slot + p - j.parts) * a.slot_rows + j.in_unit;
+}
+// the sums of every STEP-th piece from `first` on, features 4 x .. 4 x + 3
+template <int D, int STEP>
+__device__ __forceinline__ void add_pieces(const DecodeArgs &a, const JoinRow &j, int first, int x, float m, float &l, floatx4 &o)
+{
+    l = 0.0f;
+    o = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int p = group; p < all; p += G) {
-        const int64_t at = place(p);
-        const floatx2 ml = *reinterpret_cast<const floatx2 *>((p < a.p_parts ? a.part_ml : a.piece_ml) + 2 * at);
-        const floatx4 po = *reinterpret_cast<const floatx4 *>((p < a.p_parts ? a.part_o : a.piece_o) + at * D + 4 * x);
+    for (int p = first; p < j.all; p += STEP) {
+        const int64_t at = place_of(a, j, p);
+        const floatx2 ml = *reinterpret_cast<const floatx2 *>((p < j.parts ? a.part_ml : a.piece_ml) + 2 * at);
+        const floatx4 po = *reinterpret_cast<const floatx4 *>((p < j.parts ? a.part_o : a.piece_o) + at * D + 4 * x);
         if (ml[1] != 0.0f) {                               // (NaN sums go through)
             const float f = __builtin_amdgcn_exp2f(ml[0] - m);
             l += ml[1] * f;
             o += po * f;
         }
     }
-    *reinterpret_cast<floatx4 *>(&so[group][4 * x]) = o;
-    if (x == 0) sl[group] = l;
-    __syncthreads();
-    if (group != 0) return;
-    l = 0.0f;
-    o = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+// Joins parts and pieces: ROWS rows to a workgroup, D / 4 threads to a piece.  With four rows a wave joins one by itself, unless one
+// of the four has more than kFewPieces; those four, and a single row, are taken by the whole workgroup one after the other.
+// Four rows are for many units, which have two or three pieces each: 300 sequences of 10 .. 256 keys, 8 kv heads, 38 -> 32 us;
+// 1000 of 10 .. 1000 230 -> 211 us.  With 26 pieces to each of 1344 rows they are slower (39 -> 56 us).  rows_of_unit: 16 NT.
+template <int D, int ROWS>
+__global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, int rows_of_unit)
+{
+    constexpr int L = D / 4, G = kDecThreads / L;
+    __shared__ __align__(16) float so[G][D];
+    __shared__ float sl[G], sm[kDecWaves];
+    __shared__ int many;
+    const int64_t all_rows = (int64_t)a.n_seq * a.q_len * a.h_q;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (ROWS == kDecWaves) {
+        if (threadIdx.x == 0) many = 0;
+        __syncthreads();
+        const int64_t row = (int64_t)blockIdx.x * ROWS + wave;
+        JoinRow j = join_row(a, min(row, all_rows - 1), rows_of_unit);
+        if (row >= all_rows) j.done = true;
+        if (!j.done && j.all > kFewPieces && lane == 0) many = 1;
+        __syncthreads();
+        if (many == 0) {
+            if (j.done) return;
+            float m = -INFINITY, l;
+            floatx4 o;
+            if (lane < j.all) m = (lane < j.parts ? a.part_ml : a.piece_ml)[2 * place_of(a, j, lane)];
+            m = wave_max(m);
+            add_pieces<D, 64 / L>(a, j, lane / L, lane % L, m, l, o);
 #pragma unroll
-    for (int w = 0; w < G; ++w) {
-        l += sl[w];
-        o += *reinterpret_cast<const floatx4 *>(&so[w][4 * x]);
+            for (int x = L; x < 64; x <<= 1) {
+                l += __shfl_xor(l, x, 64);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) o[y] += __shfl_xor(o[y], x, 64);
+            }
+            const float out[4] = {o[0], o[1], o[2], o[3]};
+            if (lane < L) store_output(a, j.token, j.head, 4 * lane, out, m, l);
+            return;
+        }
     }
-    const float out[4] = {o[0], o[1], o[2], o[3]};
-    store_output(a, token, head, 4 * x, out, m, l);
+    for (int y = 0; y < ROWS; ++y) {
+        const int64_t row = (int64_t)blockIdx.x * ROWS + y;
+        if (row >= all_rows) return;
+        const JoinRow j = join_row(a, row, rows_of_unit);
+        if (j.done) continue;
+        float m = -INFINITY, l;
+        floatx4 o;
+        for (int p = threadIdx.x; p < j.all; p += kDecThreads) m = fmaxf(m, (p < j.parts ? a.part_ml : a.piece_ml)[2 * place_of(a, j, p)]);
+        m = wave_max(m);
+        if (lane == 0) sm[wave] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+        const int group = threadIdx.x / L, x = threadIdx.x % L;
+        add_pieces<D, G>(a, j, group, x, m, l, o);
+        *reinterpret_cast<floatx4 *>(&so[group][4 * x]) = o;
+        if (x == 0) sl[group] = l;
+        __syncthreads();
+        if (group == 0) {
+            l = 0.0f;
+            o = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < G; ++w) {
+                l += sl[w];
+                o += *reinterpret_cast<const floatx4 *>(&so[w][4 * x]);
+            }
+            const float out[4] = {o[0], o[1], o[2], o[3]};
+            store_output(a, j.token, j.head, 4 * x, out, m, l);
+        }
+        if constexpr (ROWS > 1) __syncthreads();
+    }
 }
 
 // Keys of a part of the prefix, for decode_prefix_kernel: one workgroup to a compute unit, or as few rounds of them as parts of
@@ -644,9 +710,13 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     a.p_parts = (int)p_parts;
     const long long units = (long long)a.n_seq * a.units, tiles = ((long long)a.max_len + kTileKeys - 1) / kTileKeys;
     if (p->n_seq > 65535 || units > 0x7fffffffLL - 4096) return PBS_ERR_UNSUPPORTED;
-    plan.whole = a.p_parts == 0 && a.max_len <= kWholeKeys;
+    // Lengths up to which a unit has a wave to itself and nothing is joined.  Measured, 8 kv heads, d = 128, bf16, cut to shares / whole:
+    // 64 sequences of 128 keys 16.6 / 10.2 us; of 250 keys, one 10.5 / 13.3, 300 of them 75 / 57; 1000 of 500 keys 408 / 361, but
+    // 300 of 10 .. 500 41 / 44 and 1000 of 10 .. 2000 329 / 346.
+    const int whole = units >= 4096 ? 512 : units >= 512 ? 256 : 128;
+    plan.whole = a.p_parts == 0 && a.max_len <= whole;
     // what the chip holds at a time: two workgroups to a compute unit, one where they take all registers
-    const long long most = units * (tiles + kUnitCost);
+    const long long most = units * (tiles + kUnitCost * plan.nt);
     a.shares = (plan.nt == 1 ? 512 : 256) * kDecWaves;
     if (a.shares > most) a.shares = (int)most;
     plan.grid = ((plan.whole ? units : a.max_len > 0 ? a.shares : 0) + kDecWaves - 1) / kDecWaves;
@@ -694,7 +764,10 @@ pbs_status launch_decode(const DecodePlan &plan, hipStream_t s)
         st = a.q_len == 1 ? (plan.whole ? launch_own<DTYPE, D, false, true>(plan, s) : launch_own<DTYPE, D, false, false>(plan, s))
                           : (plan.whole ? launch_own<DTYPE, D, true, true>(plan, s) : launch_own<DTYPE, D, true, false>(plan, s));
     if (st != PBS_OK || !plan.join) return st;
-    return launch(decode_join_kernel<D>, dim3((unsigned)((int64_t)a.n_seq * a.q_len * a.h_q)), dim3(kDecThreads), 0, s, a, 16 * plan.nt);
+    const int64_t rows = (int64_t)a.n_seq * a.q_len * a.h_q;
+    if (a.p_parts > 0 || a.shares > 2 * (int64_t)a.n_seq * a.units)
+        return launch(decode_join_kernel<D, 1>, dim3((unsigned)rows), dim3(kDecThreads), 0, s, a, 16 * plan.nt);
+    return launch(decode_join_kernel<D, kDecWaves>, dim3((unsigned)((rows + kDecWaves - 1) / kDecWaves)), dim3(kDecThreads), 0, s, a, 16 * plan.nt);
 }
 
 }  // namespace pbs

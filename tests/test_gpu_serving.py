@@ -264,6 +264,18 @@ def test_decode_several_new_tokens_and_head_groups(q_len, h_q, h_kv):
     s.check(O, lse)
 
 
+# units enough that a wave joins a row, or takes a whole unit; one long sequence has more pieces than a wave joins
+@pytest.mark.parametrize("n,q_len,h_q,h_kv,d,held,longest,one", [(140, 1, 8, 8, 64, "bf16", 40, 9000), (131, 1, 16, 8, 128, "e4m3", 300, 300),
+                                                                 (70, 5, 32, 8, 64, "bf16", 60, 5000), (67, 1, 16, 8, 128, "bf16", 256, 256),
+                                                                 (65, 2, 8, 8, 64, "i8", 256, 200), (515, 1, 8, 8, 64, "e4m3", 511, 512)])
+def test_decode_many_sequences(n, q_len, h_q, h_kv, d, held, longest, one):
+    lens = [(37 * i) % (longest + 1) for i in range(n)]
+    lens[n // 3] = one
+    s = Setup(5, q_len, h_q, h_kv, d, held, 32, lens)
+    O, lse = s.call(want_lse=True, max_len=max(lens))
+    s.check(O, lse)
+
+
 @pytest.mark.parametrize("held", ["bf16", "e4m3", "i8"])
 @pytest.mark.parametrize("n_seq,q_len,h_q,h_kv,d,prefix", [(1, 1, 2, 2, 64, 1), (3, 1, 8, 2, 128, 100), (9, 1, 28, 4, 128, 333), (5, 4, 8, 1, 64, 1025)])
 def test_decode_shared_prefix(n_seq, q_len, h_q, h_kv, d, prefix, held):
