@@ -527,7 +527,8 @@ __device__ __forceinline__ JoinRow join_row(const DecodeArgs &a, int64_t row, in
     const int tile = in_seq / rows_of_unit;
     const int64_t unit = (int64_t)i * a.units + tile * a.h_kv + h;
     int2 own = make_int2(0, 0);
-    if (a.shares > 0 && own_len(a, i) > 0) own = a.pieces[unit];
+    if (a.shares > 0) own = a.pieces[unit];                // undefined where there are no keys
+    if (a.shares > 0 && own_len(a, i) == 0) own = make_int2(0, 0);
     j.slot = own.x + unit;
     j.parts = a.p_parts;
     j.all = a.p_parts + own.y;
@@ -539,23 +540,50 @@ __device__ __forceinline__ int64_t place_of(const DecodeArgs &a, const JoinRow &
 {
     return p < j.parts ? p * j.all_rows + j.row : (j.slot + p - j.parts) * a.slot_rows + j.in_unit;
 }
-// the sums of every STEP-th piece from `first` on, features 4 x .. 4 x + 3
+// m, l and features 4 x .. 4 x + 3 of every STEP-th piece from `first` on: four at a time, maxima and sums read together
 template <int D, int STEP>
-__device__ __forceinline__ void add_pieces(const DecodeArgs &a, const JoinRow &j, int first, int x, float m, float &l, floatx4 &o)
+__device__ __forceinline__ void add_pieces(const DecodeArgs &a, const JoinRow &j, int first, int x, float &m, float &l, floatx4 &o)
 {
+    m = -INFINITY;
     l = 0.0f;
     o = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int p = first; p < j.all; p += STEP) {
-        const int64_t at = place_of(a, j, p);
-        const floatx2 ml = *reinterpret_cast<const floatx2 *>((p < j.parts ? a.part_ml : a.piece_ml) + 2 * at);
-        const floatx4 po = *reinterpret_cast<const floatx4 *>((p < j.parts ? a.part_o : a.piece_o) + at * D + 4 * x);
-        if (ml[1] != 0.0f) {                               // (NaN sums go through)
-            const float f = __builtin_amdgcn_exp2f(ml[0] - m);
-            l += ml[1] * f;
-            o += po * f;
+    for (int p = first; p < j.all; p += 4 * STEP) {
+        floatx2 ml[4];
+        floatx4 po[4];
+        float top = m;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int q = min(p + y * STEP, j.all - 1);
+            const int64_t at = place_of(a, j, q);
+            ml[y] = *reinterpret_cast<const floatx2 *>((q < j.parts ? a.part_ml : a.piece_ml) + 2 * at);
+            po[y] = *reinterpret_cast<const floatx4 *>((q < j.parts ? a.part_o : a.piece_o) + at * D + 4 * x);
         }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            if (p + y * STEP >= j.all) ml[y] = floatx2{-INFINITY, 0.0f};
+            top = fmaxf(top, ml[y][0]);
+        }
+        const float keep = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+        l *= keep;
+        o *= keep;
+        m = top;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+            if (ml[y][1] != 0.0f) {                        // (NaN sums go through)
+                const float f = __builtin_amdgcn_exp2f(ml[y][0] - m);
+                l += ml[y][1] * f;
+                o += po[y] * f;
+            }
     }
+}
+// two of these, into the first; nothing is a sum of zero
+__device__ __forceinline__ void add_sums(float &m, float &l, floatx4 &o, float m2, float l2, floatx4 o2)
+{
+    const float top = fmaxf(m, m2);
+    const float f = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m - top), f2 = l2 == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m2 - top);
+    l = l * f + l2 * f2;
+    o = o * f + o2 * f2;
+    m = top;
 }
 
 // Joins parts and pieces: ROWS rows to a workgroup, D / 4 threads to a piece.  With four rows a wave joins one by itself, unless one
@@ -567,7 +595,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, 
 {
     constexpr int L = D / 4, G = kDecThreads / L;
     __shared__ __align__(16) float so[G][D];
-    __shared__ float sl[G], sm[kDecWaves];
+    __shared__ float sl[G], sm[G];
     __shared__ int many;
     const int64_t all_rows = (int64_t)a.n_seq * a.q_len * a.h_q;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -581,16 +609,16 @@ __global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, 
         __syncthreads();
         if (many == 0) {
             if (j.done) return;
-            float m = -INFINITY, l;
+            float m, l;
             floatx4 o;
-            if (lane < j.all) m = (lane < j.parts ? a.part_ml : a.piece_ml)[2 * place_of(a, j, lane)];
-            m = wave_max(m);
             add_pieces<D, 64 / L>(a, j, lane / L, lane % L, m, l, o);
 #pragma unroll
             for (int x = L; x < 64; x <<= 1) {
-                l += __shfl_xor(l, x, 64);
+                const float m2 = __shfl_xor(m, x, 64), l2 = __shfl_xor(l, x, 64);
+                floatx4 o2;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) o[y] += __shfl_xor(o[y], x, 64);
+                for (int y = 0; y < 4; ++y) o2[y] = __shfl_xor(o[y], x, 64);
+                add_sums(m, l, o, m2, l2, o2);
             }
             const float out[4] = {o[0], o[1], o[2], o[3]};
             if (lane < L) store_output(a, j.token, j.head, 4 * lane, out, m, l);
@@ -602,26 +630,19 @@ __global__ __launch_bounds__(kDecThreads) void decode_join_kernel(DecodeArgs a, 
         if (row >= all_rows) return;
         const JoinRow j = join_row(a, row, rows_of_unit);
         if (j.done) continue;
-        float m = -INFINITY, l;
+        float m, l;
         floatx4 o;
-        for (int p = threadIdx.x; p < j.all; p += kDecThreads) m = fmaxf(m, (p < j.parts ? a.part_ml : a.piece_ml)[2 * place_of(a, j, p)]);
-        m = wave_max(m);
-        if (lane == 0) sm[wave] = m;
-        __syncthreads();
-        m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
         const int group = threadIdx.x / L, x = threadIdx.x % L;
         add_pieces<D, G>(a, j, group, x, m, l, o);
         *reinterpret_cast<floatx4 *>(&so[group][4 * x]) = o;
-        if (x == 0) sl[group] = l;
+        if (x == 0) {
+            sl[group] = l;
+            sm[group] = m;
+        }
         __syncthreads();
         if (group == 0) {
-            l = 0.0f;
-            o = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int w = 0; w < G; ++w) {
-                l += sl[w];
-                o += *reinterpret_cast<const floatx4 *>(&so[w][4 * x]);
-            }
+            for (int w = 1; w < G; ++w) add_sums(m, l, o, sm[w], sl[w], *reinterpret_cast<const floatx4 *>(&so[w][4 * x]));
             const float out[4] = {o[0], o[1], o[2], o[3]};
             store_output(a, j.token, j.head, 4 * x, out, m, l);
         }
