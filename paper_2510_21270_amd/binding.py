@@ -701,16 +701,19 @@ class DecodeStep:
     def capture(self, *args):
         """Record a step into a HIP graph that reads these very tensors (refill them in place, then replay()).  Q and K are
         turned by every run, the ones before the recording among them."""
-        side = torch.cuda.Stream()
-        side.wait_stream(torch.cuda.current_stream())
-        with torch.cuda.stream(side):
-            self.run(*args)
-        torch.cuda.current_stream().wait_stream(side)
-        self.graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(self.graph):
-            self.run(*args)
+        self.args = args
+        with torch.cuda.device(self.cache.K.device):
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                self.run(*args)
+            torch.cuda.current_stream().wait_stream(side)
+            self.graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(self.graph):
+                self.run(*args)
         return self.O
 
     def replay(self):
-        self.graph.replay()
+        with torch.cuda.device(self.cache.K.device):
+            self.graph.replay()
         return self.O
