@@ -332,7 +332,8 @@ typedef struct { int64_t token, head; } pbs_strides;
  *            pointers are then ignored.  Qout and Kout may be Q and K themselves with the same strides; other overlaps are
  *            not allowed.
  * The angle is formed and reduced to one turn in 64 bits; cos, sin and the products are fp32, rounded once at the end.
- * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, rot, layout, more than 2^31 - 1 rows), PBS_ERR_HIP.
+ * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, rot, layout, h_q + h_kv > 8192, more than 2^31 - 1
+ * rows), PBS_ERR_HIP.
  */
 enum { PBS_ROPE_HALF = 0, PBS_ROPE_INTERLEAVED = 1 };
 enum { PBS_ROPE_TRANSPOSE = 1u };
@@ -390,7 +391,8 @@ typedef struct {
  * pbs_cache_read is the way back: row t of K, V [tokens, h_kv, d] of `dtype` becomes what slot slots[t] stands for
  * (the held value times its factor in fp32, rounded to dtype), zeros for a slot outside the cache.  K or V may be NULL
  * (then it is not read back); slots may repeat.
- * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, page, too many slots or rows), PBS_ERR_HIP.
+ * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, page, h_kv > 65535, more than 2^31 - 1 slots or
+ * 2^31 - 256 rows), PBS_ERR_HIP.
  */
 pbs_status pbs_cache_write(const pbs_cache *c, int32_t dtype, int32_t tokens, const void *K, const pbs_strides *k,
                            const void *V, const pbs_strides *v, const int32_t *slots, void *stream);

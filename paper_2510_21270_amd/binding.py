@@ -645,6 +645,8 @@ class Pipeline:
         """With a `cache` the keys and values also go into its slots [batch, n], for the decode steps behind the prompt."""
         p = self.p
         if cache is not None:
+            if slots is None or slots.shape != (p.batch, p.n):
+                _refuse("pbs_cache_write", "a cache needs slots [batch, n]")
             for b in range(p.batch):
                 cache_write(cache, K[b].transpose(0, 1), V[b].transpose(0, 1), slots[b])
         key_scores(p, Q, K, self.scores, self.ws1)

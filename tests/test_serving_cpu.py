@@ -236,3 +236,12 @@ def test_prompt_refusals(lib):
     p = prob()
     p.k = b.pbs_strides(130, 64)
     assert call(p) == 2
+
+
+def test_a_pipeline_refuses_a_cache_without_slots():
+    p = b.problem(batch=1, h_q=2, h_kv=1, n=256, d=128, block=128, segment=256, dtype="bf16", tau=0.9)
+    pipe = b.Pipeline(p, device="cpu")
+    x = torch.zeros(1, 2, 256, 128, dtype=torch.bfloat16)
+    for slots in (None, torch.zeros(256, dtype=torch.int32), torch.zeros(1, 255, dtype=torch.int32)):
+        with pytest.raises(b.PbsError, match="slots"):
+            pipe.run(x, x[:, :1], x[:, :1], cache=object(), slots=slots)
