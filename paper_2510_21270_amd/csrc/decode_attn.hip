@@ -314,6 +314,13 @@ __device__ __forceinline__ int tiles_of(const DecodeArgs &a, int i) { return cei
 template <int NT>
 __device__ __forceinline__ int cost_of(int n) { return n > 0 ? n + kUnitCost * NT : 0; }
 
+// of numbers that are not negative; most have 32 bits, whose division takes a third of the instructions
+__device__ __forceinline__ int64_t quotient64(int64_t x, int64_t y)
+{
+    if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
+    return x / y;
+}
+
 // Sum over the workgroup, and in `before` the sum over the threads in front of this one.
 __device__ __forceinline__ int scan_group(int v, int &before, int *sums)
 {
@@ -386,46 +393,67 @@ __global__ __launch_bounds__(kDecThreads, NT == 1 ? 2 : 1) void decode_own_kerne
             own_piece<DTYPE, D, NT, SEVERAL>(a, i, w - i * a.units, len, 0, ceil_div(len, kTileKeys), 0, true);
         return;
     }
-    __shared__ int sums[kDecWaves], found[kDecWaves];
-    __shared__ int64_t found_front[kDecWaves];
-    int64_t total = 0;
-    int before;
-    for (int base = 0; base < a.n_seq; base += kDecThreads) {
-        const int x = base + threadIdx.x;
-        total += scan_group(x < a.n_seq ? cost_of<NT>(tiles_of(a, x)) : 0, before, sums);
-    }
-    const int64_t share = max((total * a.units + a.shares - 1) / a.shares, (int64_t)1), all = total * a.units;
-    // the sequence that each wave's share begins in, and the cost of those in front of it
-    int64_t front = 0;
-    for (int base = 0; base < a.n_seq; base += kDecThreads) {
-        const int x = base + threadIdx.x, n = x < a.n_seq ? cost_of<NT>(tiles_of(a, x)) : 0;
-        const int sum = scan_group(n, before, sums);
-        const int64_t mine = (front + before) * a.units;
-#pragma unroll
-        for (int y = 0; y < kDecWaves; ++y) {
-            const int64_t at = (int64_t)(blockIdx.x * kDecWaves + y) * share;
-            if (mine <= at && at < mine + (int64_t)n * a.units) {
-                found[y] = x;
-                found_front[y] = mine;
-            }
+    int64_t total = 0, share, all, at, front;
+    int i, len;
+    if (a.n_seq <= 64) {                                   // every wave for itself, a lane to a sequence
+        const int lane = threadIdx.x & 63, mine = lane < a.n_seq ? own_len(a, lane) : 0, v = cost_of<NT>(ceil_div(mine, kTileKeys));
+        int sum = v;
+        for (int o = 1; o < a.n_seq; o <<= 1) {
+            const int other = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += other;
         }
-        front += sum;
+        total = __builtin_amdgcn_readlane(sum, a.n_seq - 1);
+        all = total * a.units;
+        share = max(quotient64(all + a.shares - 1, a.shares), (int64_t)1);
+        at = w * share;
+        if (at >= all) return;
+        i = __builtin_ctzll(__ballot(lane < a.n_seq && at < (int64_t)sum * a.units));
+        len = __builtin_amdgcn_readlane(mine, i);
+        front = (int64_t)__builtin_amdgcn_readlane(sum - v, i) * a.units;
+    } else {
+        __shared__ int sums[kDecWaves], found[kDecWaves];
+        __shared__ int64_t found_front[kDecWaves];
+        int before;
+        for (int base = 0; base < a.n_seq; base += kDecThreads) {
+            const int x = base + threadIdx.x;
+            total += scan_group(x < a.n_seq ? cost_of<NT>(tiles_of(a, x)) : 0, before, sums);
+        }
+        all = total * a.units;
+        share = max(quotient64(all + a.shares - 1, a.shares), (int64_t)1);
+        // the sequence that each wave's share begins in, and the cost of those in front of it
+        front = 0;
+        for (int base = 0; base < a.n_seq; base += kDecThreads) {
+            const int x = base + threadIdx.x, n = x < a.n_seq ? cost_of<NT>(tiles_of(a, x)) : 0;
+            const int sum = scan_group(n, before, sums);
+            const int64_t mine = (front + before) * a.units;
+#pragma unroll
+            for (int y = 0; y < kDecWaves; ++y) {
+                const int64_t begin = (int64_t)(blockIdx.x * kDecWaves + y) * share;
+                if (mine <= begin && begin < mine + (int64_t)n * a.units) {
+                    found[y] = x;
+                    found_front[y] = mine;
+                }
+            }
+            front += sum;
+        }
+        __syncthreads();
+        at = w * share;
+        if (at >= all) return;
+        i = __builtin_amdgcn_readfirstlane(found[wave]);
+        len = __builtin_amdgcn_readfirstlane(own_len(a, i));
+        front = found_front[wave];
     }
-    __syncthreads();
-    int64_t at = w * share;
     const int64_t stop = min(at + share, all);
-    if (at >= stop) return;
-    int i = __builtin_amdgcn_readfirstlane(found[wave]);
-    int len = __builtin_amdgcn_readfirstlane(own_len(a, i)), n = ceil_div(len, kTileKeys), cost = cost_of<NT>(n);
-    const int64_t inside = at - found_front[wave];         // of the sequence's units, in tiles
-    int k = __builtin_amdgcn_readfirstlane((int)(inside / cost)), off = __builtin_amdgcn_readfirstlane((int)(inside - (int64_t)k * cost));
+    int n = ceil_div(len, kTileKeys), cost = cost_of<NT>(n);
+    const int64_t inside = at - front;                     // of the sequence's units, in tiles
+    int k = __builtin_amdgcn_readfirstlane((int)quotient64(inside, cost)), off = __builtin_amdgcn_readfirstlane((int)(inside - (int64_t)k * cost));
     while (true) {
         const int take = (int)min((int64_t)(cost - off), stop - at);
         const int first = max(off - kUnitCost * NT, 0), last = off + take - kUnitCost * NT;             // tiles
         const int64_t unit = (int64_t)i * a.units + k, slot = w + unit;       // one of the two moves on with every piece
         if (last > first) {
             if (first == 0 && (threadIdx.x & 63) == 0)
-                a.pieces[unit] = make_int2(w, (int)((at - off + cost - 1) / share) - w + 1);
+                a.pieces[unit] = make_int2(w, (int)quotient64(at - off + cost - 1, share) - w + 1);
             own_piece<DTYPE, D, NT, SEVERAL>(a, i, k, len, first, last, slot, first == 0 && last == n && a.p_parts == 0);
         }
         at += take;
