@@ -549,8 +549,8 @@ __device__ __forceinline__ JoinRow join_row(const DecodeArgs &a, int64_t row, in
     JoinRow j;
     j.row = row;
     j.all_rows = (int64_t)a.n_seq * a.q_len * a.h_q;
-    j.token = (int)(row / a.h_q);
-    j.head = (int)(row - (int64_t)j.token * a.h_q);
+    j.token = (int)((uint32_t)row / (uint32_t)a.h_q);      // fewer than 2^31 rows
+    j.head = (int)row - j.token * a.h_q;
     const int i = j.token / a.q_len, h = j.head / a.r, in_seq = (j.token - i * a.q_len) * a.r + j.head - h * a.r;
     const int tile = in_seq / rows_of_unit;
     const int64_t unit = (int64_t)i * a.units + tile * a.h_kv + h;
