@@ -3,7 +3,8 @@
 // y = magnitude * R(position * f_e) x on every pair of features.  Bytes bound it: 3 operations to a feature that is read and
 // written once.  A workgroup takes a few tokens: its threads form the tokens' angles once (fp64 product in turns, the
 // whole turns taken off in fp64, which is exact, cos and sin of what is left in fp32) into LDS and then walk over the rows of
-// all heads, 16 features to a thread and step, so that a wave moves consecutive memory.
+// all heads, 16 features to a thread and step, so that a wave moves consecutive memory.  32768 tokens of 32 + 8 heads of 128 in bf16:
+// 114 us, 5.9 TB/s read and written; a step of 32 tokens: 3.4 us.
 #include "pbs_host.h"
 #include "serving.h"
 
@@ -117,18 +118,12 @@ extern "C" pbs_status pbs_rope(const pbs_rope_problem *p, const double *freq, co
 
     RopeArgs a;
     a.tokens = p->tokens; a.h_q = p->h_q; a.heads = (int)heads; a.d = p->d; a.rot = p->rot;
-    // As many tokens to a workgroup as fill the threads' last round best (32 + 8 heads of 128: 4, five full rounds), while there
-    // are workgroups for every compute unit several times over.
+    // As many tokens to a workgroup as its threads have an item each of, while there are workgroups for every compute unit several
+    // times over.  Measured in bf16 with 1 / 2 / 4 / 8 tokens: 32768 x (32 + 8) heads of 128, 320 items to a token, 114 / 121 / 126 /
+    // 134 us (5.9 TB/s with one); with 1 / 2 / 3 / 8 for 16 + 4 heads of 64, 80 items, 31.3 / 26.1 / 26.3 / 27.0 us.
+    const long long items = heads * (p->d / 16);
     a.per_wg = 1;
-    double full = 0.0;
-    for (int n = 1; n <= kRopeTokens && p->tokens >= 1024 * n && heads * n <= 4096; ++n) {
-        const long long items = n * heads * (p->d / 16), rounds = (items + kRopeThreads - 1) / kRopeThreads;
-        const double share = (double)items / (double)(rounds * kRopeThreads);
-        if (share > full + 0.02) {
-            full = share;
-            a.per_wg = n;
-        }
-    }
+    while (a.per_wg < kRopeTokens && (a.per_wg + 1) * items <= kRopeThreads && p->tokens >= 1024 * (a.per_wg + 1)) ++a.per_wg;
     a.head_magic = (unsigned)((0x100000000ull + heads - 1) / heads);
     a.magnitude = p->magnitude == 0.0f ? 1.0f : p->magnitude;
     a.sign = (p->flags & PBS_ROPE_TRANSPOSE) ? -1.0f : 1.0f;
