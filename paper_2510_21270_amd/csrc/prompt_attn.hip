@@ -39,12 +39,9 @@ __device__ __forceinline__ Place find_place(const Args &a, int b, int lane)
         }
         const int tiles = (len_q + a.tokens - 1) / a.tokens;
         int sum = tiles;
-        if (a.n_seq > 1) {
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int other = __shfl_up(sum, o, 64);
-                if (lane >= o) sum += other;
-            }
+        for (int o = 1; o < min(a.n_seq - base, 64); o <<= 1) {
+            const int other = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += other;
         }
         const unsigned long long has = __ballot(i < a.n_seq && b < sum);
         if (has) {
