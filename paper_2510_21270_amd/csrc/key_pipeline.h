@@ -143,6 +143,18 @@ __device__ __forceinline__ void meet()
     __syncthreads();
 }
 
+// the same but for this wave's newest N loads
+template <int N>
+__device__ __forceinline__ void meet_but()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int D>
 struct State {
     floatx16 o[D / 32][2];
@@ -531,14 +543,17 @@ __device__ __forceinline__ void all_tiles(State<D> &st, bf16x8 (&q)[2][D / 16], 
     const int h = lane >> 5;
     // stage p: K tile p, V tile p - 1; the V tile of stage 0, number 3, comes again in iteration 0: zero weights need some values
     issue_tile(sg0, src, off, wave == 0 ? 0 : 3, wave);
-    issue_tile(sg1, src, off, wave == 0 ? 1 : 0, wave);
-    issue_tile(sg2, src, off, wave == 0 ? 2 : 1, wave);
-    issue_tile(sg3, src, off, wave == 0 ? 3 : 2, wave);
     issue_factors(sg0, src, 0, wave, lane);
-    issue_factors(sg1, src, 1, wave, lane);
-    issue_factors(sg2, src, 2, wave, lane);
+    __builtin_amdgcn_sched_barrier(0);
     load_queries();
-    meet();
+    __builtin_amdgcn_sched_barrier(0);
+    issue_tile(sg1, src, off, wave == 0 ? 1 : 0, wave);
+    issue_factors(sg1, src, 1, wave, lane);
+    issue_tile(sg2, src, off, wave == 0 ? 2 : 1, wave);
+    issue_factors(sg2, src, 2, wave, lane);
+    issue_tile(sg3, src, off, wave == 0 ? 3 : 2, wave);
+    constexpr int kEach = Offsets<D>::kLoads + (F ? 1 : 0);
+    meet_but<2 * kEach + Offsets<D>::kLoads>();            // the first tile and the queries are there
     floatx16 sa[2], sb[2];
     bf16x8 kf[D / 16], pa[2][2], pb[2][2];
 #pragma unroll
@@ -569,6 +584,7 @@ __device__ __forceinline__ void all_tiles(State<D> &st, bf16x8 (&q)[2][D / 16], 
                 for (int e = 0; e < 8; ++e) pa[nt][u][e] = (bf16_t)0.0f;
         }
     }
+    meet_but<kEach + Offsets<D>::kLoads>();                // the second one
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) kf[x] = *reinterpret_cast<const bf16x8 *>(sg1.k + off.kf[x]);
     __builtin_amdgcn_sched_barrier(0);

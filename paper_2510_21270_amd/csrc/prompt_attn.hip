@@ -32,10 +32,12 @@ __device__ __forceinline__ Place find_place(const Args &a, int b, int lane)
         const int i = base + lane;
         int q0 = 0, len_q = 0, k0 = 0, len_k = 0;
         if (i < a.n_seq) {
-            q0 = min(max(a.cu_q[i], 0), a.total_q);
-            len_q = max(min(max(a.cu_q[i + 1], 0), a.total_q) - q0, 0);
-            k0 = min(max(a.cu_k[i], 0), a.total_k);
-            len_k = max(min(max(a.cu_k[i + 1], 0), a.total_k) - k0, 0);
+            int qa = a.cu_q[i], qb = a.cu_q[i + 1], ka = a.cu_k[i], kb = a.cu_k[i + 1];
+            asm volatile("" : "+v"(qa), "+v"(qb), "+v"(ka), "+v"(kb));         // one wait for all four
+            q0 = min(max(qa, 0), a.total_q);
+            len_q = max(min(max(qb, 0), a.total_q) - q0, 0);
+            k0 = min(max(ka, 0), a.total_k);
+            len_k = max(min(max(kb, 0), a.total_k) - k0, 0);
         }
         const int tiles = (len_q + a.tokens - 1) / a.tokens;
         int sum = tiles;
