@@ -3,7 +3,7 @@
 //
 // A bf16 cache is read where its pages lie.  8-bit values are first written out as bf16, in order, the factors beside them: the
 // pipeline has no room for the widening of every tile in every workgroup, and the prefix is short beside what is done with it.
-// What bounds it is the start and the end of the workgroups, about 8 us, where a part has few tiles (48 answers to 8147 keys, 28 heads
+// What bounds it is the start and the end of the workgroups, about 7 us, where a part has few tiles (48 answers to 8147 keys, 28 heads
 // on 4 of 128, bf16: 20 us for 5.7 GFLOP), the pipeline from some ten thousand keys on.
 #include "decode.h"
 #include "key_pipeline.h"
