@@ -363,7 +363,7 @@ _ROPE = struct.Struct("7ifI8q").pack
 _CACHE = struct.Struct("5i4P").pack
 _DECODE = struct.Struct("7if4q").pack
 _PROMPT = struct.Struct("7ifI8q").pack
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _refuse(what, why):
