@@ -403,7 +403,7 @@ pbs_status pbs_cache_read(const pbs_cache *c, int32_t dtype, int32_t tokens, con
  * Attention of each sequence's newest q_len tokens over its cached keys, a prefix that all sequences share in front of
  * them: query t of sequence i sees all prefix_len prefix keys and its own keys 0 .. lens[i] - q_len + t (its own keys
  * include the new tokens, written before this call).  O = softmax(scale * Q K^T) V over these; a query that sees none gets a
- * zero row and lse = -inf.
+ * zero row and lse = -inf, as does one whose logits are all -inf.
  *   Q, O     token i * q_len + t; dtype bf16 whatever the cache holds; h_q % c->h_kv == 0.  O may be Q itself.
  *   page_table [n_seq, max_pages] int32: the pages of a sequence's own keys in order; entries behind its length are
  *            not looked at.  A listed page outside [0, pages) counts as keys that nobody sees.
@@ -438,7 +438,7 @@ pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cache *c, cons
  * [0, total_k] is taken as the nearest inside, a length below zero as zero).  With PBS_PROMPT_CAUSAL query t of a sequence sees
  * key j iff j <= t + (number of keys) - (number of queries): the newest query sees everything, as when a chunk of a
  * prompt follows keys that are there already; without it every query sees every key of its sequence.  A query that sees no
- * key gets a zero row and lse = -inf.  Rows of O and lse that belong to no sequence stay as they were.
+ * key, or whose logits are all -inf, gets a zero row and lse = -inf.  Rows of O and lse that belong to no sequence stay as they were.
  *   Q, O [total_q, h_q, d], K, V [total_k, h_kv, d], bf16; h_q % h_kv == 0, h_q / h_kv <= 128; lse [total_q, h_q] float32 or NULL.
  *   O may not overlap Q, K or V.
  * Probabilities enter the second product in bf16, everything else is fp32.

@@ -691,3 +691,21 @@ def test_prompt_on_another_stream_and_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(O, pbs.prompt_attn(Q, K, V, cu))
+
+
+@pytest.mark.parametrize("prefix", [0, 40])
+def test_logits_that_are_all_minus_infinity_count_as_no_key(prefix):
+    s = Setup(40, 1, 4, 1, 64, "bf16", 16, [50, 500], prefix)
+    s.cache.K[..., 0] = -3e38
+    s.Q[:, :, 2, 0] = 3e38                                 # their product leaves float32's range
+    s.Q[:, :, [0, 1, 3], 0] = 0
+    O, lse = s.call(want_lse=True)
+    assert not O[:, :, 2].any() and bool((lse[:, :, 2] == -math.inf).all())
+    assert bool(torch.isfinite(lse[:, :, [0, 1, 3]]).all()) and bool(torch.isfinite(O.float()).all())
+    Q, K, V, cu, _ = _prompts(41, [70, 300], [0, 0], 4, 1, 64)
+    K[..., 0] = -3e38
+    Q[:, 2, 0] = 3e38
+    Q[:, [0, 1, 3], 0] = 0
+    O, lse = pbs.prompt_attn(Q.cuda(), K.cuda(), V.cuda(), cu.cuda(), want_lse=True)
+    assert not O[:, 2].any() and bool((lse[:, 2] == -math.inf).all())
+    assert bool(torch.isfinite(lse[:, [0, 1, 3]]).all()) and bool(torch.isfinite(O.float()).all())
