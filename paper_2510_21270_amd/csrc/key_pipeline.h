@@ -79,19 +79,20 @@ __device__ __forceinline__ Offsets<D> offsets(int wave, int lane, uint32_t strid
     return r;
 }
 
-// What a wave brings, wave 0 K and wave 1 V, from consecutive rows (the factors beside them, F).  A tile that starts behind the
-// end starts at the end, where reads give zeros.
+// What a wave brings, wave 0 K and wave 1 V, from consecutive rows (the factors beside them, F).  A tile behind the
+// last one starts at the end, where reads give zeros.
 template <int D, bool F>
 struct Rows {
     __amdgpu_buffer_rsrc_t rows, factors;
-    int size, tile_bytes, factors_size;
+    int size, tiles, tile_bytes, factors_size;
     struct At {
         int rows;
         __device__ __forceinline__ void pin() { asm volatile("" : "+s"(rows)); }
     };
     __device__ __forceinline__ At at(int t) const
     {
-        return {scalar_offset(t * tile_bytes, size)};
+        if constexpr (F) return {scalar_offset(t * tile_bytes, size)};         // (a part of a prefix: a thousand rows of 256 bytes)
+        else return {tile_start(t, tiles, tile_bytes, size)};
     }
     __device__ __forceinline__ void load(unsigned char *dst, int c, const At &w, const Offsets<D> &off) const
     {

@@ -15,4 +15,14 @@ constexpr int listed_slot(int j, int part, int step, int block, int ni, int n)
 // scalar offset, a difference that must not fall below zero.
 constexpr int scalar_offset(int at, int size) { return at < size ? at : size; }
 
+// The same of tile t of `tiles`, tile_bytes each.  A pipeline that brings tiles ahead asks for some behind the last one, whose
+// product may not have 31 bits; rows_have_places says that the others have.
+constexpr int tile_start(int t, int tiles, int tile_bytes, int size) { return t < tiles ? t * tile_bytes : size; }
+
+// Whether the offsets in `rows` rows of row_bytes, step_bytes apart, and in a tile that starts behind them, have 31 bits.
+constexpr bool rows_have_places(long long rows, int tile, long long step_bytes, int row_bytes)
+{
+    return (rows + 2 * tile) * step_bytes + row_bytes < 0x80000000ll;
+}
+
 }  // namespace pbs

@@ -134,6 +134,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     Rows<D, false> src;
     src.rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(base), 0, size, 0x00020000);
     src.size = size;
+    src.tiles = (pl.len_k + KS - 1) / KS;
     src.tile_bytes = KS * step_bytes;
     const Offsets<D> off = offsets<D>(wave, lane, (uint32_t)step_bytes);
     if (threadIdx.x == 0) bad_rows = 0;
@@ -179,9 +180,9 @@ extern "C" pbs_status pbs_prompt_attn(const pbs_prompt_problem *p, const void *Q
     if (p->total_k > 0 && (!good_input(K, p->k, 2) || !good_input(V, p->v, 2))) return PBS_ERR_SHAPE;
     if (((reinterpret_cast<uintptr_t>(cu_q) | reinterpret_cast<uintptr_t>(cu_k) | reinterpret_cast<uintptr_t>(lse)) & 3u) != 0)
         return PBS_ERR_SHAPE;
-    // byte offsets inside a head's rows, a tile past the end included, are 31 bits
+    // byte offsets inside a head's rows have 31 bits
     const long long stride = p->k.token > p->v.token ? p->k.token : p->v.token;
-    if (((long long)p->total_k + 2 * prompt::KS) * stride * 2 + p->d * 2 >= 0x80000000ll) return PBS_ERR_UNSUPPORTED;
+    if (!rows_have_places(p->total_k, prompt::KS, stride * 2, p->d * 2)) return PBS_ERR_UNSUPPORTED;
     const long long grid = ((long long)p->total_q / tokens + p->n_seq) * p->h_kv;
     if (grid > 0x7fffffffLL) return PBS_ERR_UNSUPPORTED;
 
