@@ -7,6 +7,7 @@ import re
 import subprocess
 
 from paper_2510_21270_amd import build
+from test_load_places_cpu import SCALAR_OFFSET, WITHIN as LOOKED_AT, _arguments
 
 
 def _source(name):
@@ -80,3 +81,34 @@ int main()
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", build.CSRC, src, "-o", exe], check=True)
     out = subprocess.run([exe], check=True, stdout=subprocess.PIPE, text=True).stdout
     assert "all places hold" in out
+
+
+# scalar offsets by which no load of the pipeline starts behind its descriptor, and why; the other files' stand in
+# test_load_places_cpu.py
+WITHIN = {
+    "key_pipeline.h": {
+        "w.rows": "Rows::at forms it by tile_start, or scalar_offset",
+        "scalar_offset(t * KS * 4, factors_size)": "stops at the end",
+    },
+    "prefix_attn.hip": {},                                 # a descriptor to every tile
+}
+
+
+def test_no_load_of_the_pipeline_starts_behind_its_descriptor():
+    for name, known in WITHIN.items():
+        text, found = _source(name), 0
+        for m in re.finditer(r"\b(%s)\(" % "|".join(SCALAR_OFFSET), text):
+            offset = " ".join(_arguments(text, m.end() - 1)[SCALAR_OFFSET[m.group(1)]].split())
+            found += 1
+            assert offset == "0" or offset in known, (name, offset)
+        assert found, name
+
+
+def test_every_file_with_buffer_loads_is_looked_at():
+    for name in sorted(os.listdir(build.CSRC)):
+        if not name.endswith((".hip", ".h")):
+            continue
+        loads = set(re.findall(r"\b__builtin_amdgcn_(?:raw|struct)_\w*buffer_load\w*", _source(name)))
+        assert not loads or name in WITHIN or name in LOOKED_AT, name
+        assert loads <= set(SCALAR_OFFSET), (name, loads)  # each with a known place of its scalar offset
+        assert "buffer_load" not in re.sub(r"__builtin_amdgcn_\w+", "", _source(name)), name
