@@ -404,7 +404,8 @@ pbs_status pbs_cache_read(const pbs_cache *c, int32_t dtype, int32_t tokens, con
  * them: query t of sequence i sees all prefix_len prefix keys and its own keys 0 .. lens[i] - q_len + t (its own keys
  * include the new tokens, written before this call).  O = softmax(scale * Q K^T) V over these; a query that sees none gets a
  * zero row and lse = -inf, as does one whose logits are all -inf.
- *   Q, O     token i * q_len + t; dtype bf16 whatever the cache holds; h_q % c->h_kv == 0.  O may be Q itself.
+ *   Q, O     token i * q_len + t; dtype bf16 whatever the cache holds; h_q % c->h_kv == 0.  O may be Q itself with
+ *            the same strides (PBS_ERR_SHAPE otherwise); other overlaps are not allowed.
  *   page_table [n_seq, max_pages] int32: the pages of a sequence's own keys in order; entries behind its length are
  *            not looked at.  A listed page outside [0, pages) counts as keys that nobody sees.
  *   lens     [n_seq] int32, device memory: own keys; negative counts as 0, more than min(max_len, max_pages * page) as that.
@@ -440,7 +441,7 @@ pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cache *c, cons
  * prompt follows keys that are there already; without it every query sees every key of its sequence.  A query that sees no
  * key, or whose logits are all -inf, gets a zero row and lse = -inf.  Rows of O and lse that belong to no sequence stay as they were.
  *   Q, O [total_q, h_q, d], K, V [total_k, h_kv, d], bf16; h_q % h_kv == 0, h_q / h_kv <= 128; lse [total_q, h_q] float32 or NULL.
- *   O may not overlap Q, K or V.
+ *   O may not overlap Q, K or V (PBS_ERR_SHAPE where it starts at one of them).
  * Probabilities enter the second product in bf16, everything else is fp32.
  * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, h_q / h_kv > 128, rows beyond 2^31 - 1, a grid that is
  * too large, K or V of one head spanning 2 GiB or more), PBS_ERR_HIP.

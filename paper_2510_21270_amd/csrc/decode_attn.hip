@@ -847,6 +847,8 @@ extern "C" pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cac
     if (((reinterpret_cast<uintptr_t>(page_table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(prefix_pages) |
           reinterpret_cast<uintptr_t>(lse)) & 3u) != 0)
         return PBS_ERR_SHAPE;
+    // a wave stores where it has read its own queries; with other strides it would store over another's (an axis of one has no stride)
+    if (Q == O && ((p->q.head != p->o.head && p->h_q > 1) || (p->q.token != p->o.token && (long long)p->n_seq * p->q_len > 1))) return PBS_ERR_SHAPE;
     if (plan.bytes > 0) {
         if (!ws) return PBS_ERR_NULL;
         if ((reinterpret_cast<uintptr_t>(ws) & (kWsAlign - 1)) != 0 || ws_bytes < plan.bytes) return PBS_ERR_WORKSPACE;

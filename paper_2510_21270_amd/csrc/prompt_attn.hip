@@ -185,6 +185,7 @@ extern "C" pbs_status pbs_prompt_attn(const pbs_prompt_problem *p, const void *Q
     if (!rows_have_places(p->total_k, prompt::KS, stride * 2, p->d * 2)) return PBS_ERR_UNSUPPORTED;
     const long long grid = ((long long)p->total_q / tokens + p->n_seq) * p->h_kv;
     if (grid > 0x7fffffffLL) return PBS_ERR_UNSUPPORTED;
+    if (O == Q || (p->total_k > 0 && (O == K || O == V))) return PBS_ERR_SHAPE;              // rows may be formed a second time
 
     prompt::Args a;
     a.n_seq = p->n_seq; a.total_q = p->total_q; a.total_k = p->total_k;
