@@ -660,7 +660,8 @@ class Pipeline:
     def capture(self, Q, K, V, qidx=None, cache=None, slots=None):
         """Record the pipeline into a HIP graph that reads these very tensors (refill them in place, then replay()).
         The library allocates nothing, never synchronises and records no memset nodes, so the calls can be captured
-        as they are; short sequences, where the dozen launches cost more than the kernels, gain from it."""
+        as they are; short sequences, where the dozen launches cost more than the kernels, gain from it.  The tensors and
+        the cache live as long as the graph does."""
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
@@ -669,6 +670,7 @@ class Pipeline:
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
             self._graph_out = self.run(Q, K, V, qidx, cache, slots)
+        self._graph_args = (Q, K, V, qidx, cache, slots)   # the graph has their addresses only
         return self._graph_out
 
     def replay(self):
