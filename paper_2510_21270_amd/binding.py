@@ -667,10 +667,11 @@ class Pipeline:
         with torch.cuda.stream(side):
             self.run(Q, K, V, qidx, cache, slots)          # everything lazily initialised happens outside the capture
         torch.cuda.current_stream().wait_stream(side)
-        self.graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(self.graph):
-            self._graph_out = self.run(Q, K, V, qidx, cache, slots)
-        self._graph_args = (Q, K, V, qidx, cache, slots)   # the graph has their addresses only
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = self.run(Q, K, V, qidx, cache, slots)
+        # a graph has addresses only; one that could not be recorded leaves the former one and its tensors
+        self.graph, self._graph_out, self._graph_args = graph, out, (Q, K, V, qidx, cache, slots)
         return self._graph_out
 
     def replay(self):
@@ -705,16 +706,16 @@ class DecodeStep:
     def capture(self, *args):
         """Record a step into a HIP graph that reads these very tensors (refill them in place, then replay()).  Q and K are
         turned by every run, the ones before the recording among them."""
-        self.args = args
         with torch.cuda.device(self.cache.K.device):
             side = torch.cuda.Stream()
             side.wait_stream(torch.cuda.current_stream())
             with torch.cuda.stream(side):
                 self.run(*args)
             torch.cuda.current_stream().wait_stream(side)
-            self.graph = torch.cuda.CUDAGraph()
-            with torch.cuda.graph(self.graph):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
                 self.run(*args)
+        self.graph, self.args = graph, args                # a graph has addresses only
         return self.O
 
     def replay(self):

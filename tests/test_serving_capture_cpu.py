@@ -67,3 +67,29 @@ def test_a_recorded_graph_keeps_its_tensors(recording, monkeypatch, make, n):
     owner.capture(*_inputs(n))                             # the next recording lets them go
     gc.collect()
     assert all(r() is None for r in refs)
+
+
+@pytest.mark.parametrize("make,n", [(_pipeline, 6), (_step, 7)])
+@pytest.mark.parametrize("fails", ["before", "while"])
+def test_a_recording_that_fails_leaves_the_former_one(recording, monkeypatch, make, n, fails):
+    owner, first = make(), torch.zeros(1)
+    monkeypatch.setattr(owner, "run", lambda *a: first)
+    args = _inputs(n)
+    refs = [weakref.ref(x) for x in args]
+    owner.capture(*args)
+    graph = owner.graph
+    del args
+    calls = []
+
+    def run(*a):
+        calls.append(1)
+        if len(calls) == (1 if fails == "before" else 2):
+            raise b.PbsError("refused")
+        return torch.zeros(1)
+
+    monkeypatch.setattr(owner, "run", run)
+    with pytest.raises(b.PbsError, match="refused"):
+        owner.capture(*_inputs(n))
+    gc.collect()
+    assert owner.graph is graph and all(r() is not None for r in refs)
+    assert owner.replay() is (first if make is _pipeline else owner.O) and graph.replays == 1
