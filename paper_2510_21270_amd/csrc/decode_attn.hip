@@ -761,7 +761,7 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
         if (a.p_chunk < 128) a.p_chunk = 128;
     }
     const int64_t p_parts = ((int64_t)a.prefix_len + a.p_chunk - 1) / a.p_chunk;
-    if (p_parts > 65535 || a.p_row_tiles > 65535) return PBS_ERR_UNSUPPORTED;
+    if (p_parts > 65535 || (p_parts > 0 && a.p_row_tiles > 65535)) return PBS_ERR_UNSUPPORTED;
     a.p_parts = (int)p_parts;
     const long long units = (long long)a.n_seq * a.units, tiles = ((long long)a.max_len + kTileKeys - 1) / kTileKeys;
     if (p->n_seq > 65535 || units > 0x7fffffffLL - 4096) return PBS_ERR_UNSUPPORTED;

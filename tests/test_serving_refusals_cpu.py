@@ -37,3 +37,17 @@ def test_packed_prompts_are_not_attended_to_in_place(lib):
 
     for O in (1 << 16, 1 << 17, 1 << 18):
         assert call(1 << 16, 1 << 17, 1 << 18, O) == 2
+
+
+def test_the_prefix_limits_rows_only_where_there_is_one(lib):
+    # 60000 sequences of 16 new tokens: more rows than the grid of a prefix holds, which is not launched without one
+    c = _cache(h_kv=2)
+    p = _decode(n_seq=60000, q_len=16, h_q=32, max_pages=5, max_len=80)
+    p.q = p.o = b.pbs_strides(32 * 64, 64)
+    need = lib.pbs_decode_workspace_bytes(ctypes.byref(p), ctypes.byref(c))
+    assert need == 0                                       # a wave to a unit
+    assert _decode_call(lib, p, c, 4096, 4096 + 8) == 2    # the next check
+    p.max_pages = p.max_len = 1000
+    assert lib.pbs_decode_workspace_bytes(ctypes.byref(p), ctypes.byref(c)) > 0
+    p.prefix_len = 100
+    assert lib.pbs_decode_workspace_bytes(ctypes.byref(p), ctypes.byref(c)) == 0 and _decode_call(lib, p, c, 4096, 4096) == 3
