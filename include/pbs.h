@@ -313,7 +313,9 @@ pbs_status pbs_shader_clock_meter(float *out, int micros, void *stream);
  * h * strides.head + e, in elements; features are consecutive.  [tokens, heads, d] memory has strides {heads * d, d}, the
  * [1, heads, n, d] memory of the calls above {d, n * d}, and a slice of a fused projection its own.  Base addresses are
  * 16-byte aligned, strides are not negative, below 2^31 and whole multiples of 16 bytes; rows of an output do not overlap (all
- * PBS_ERR_SHAPE otherwise).  d is 64 or 128.  A count of zero tokens or sequences is a call that does nothing.
+ * PBS_ERR_SHAPE otherwise).  d is 64 or 128.  A count of zero tokens or sequences is a call that does nothing.  A launch has
+ * fewer than 2^32 threads: a call that needs more of a kernel is PBS_ERR_UNSUPPORTED (pbs_rope from 2^24 workgroups of one to
+ * eight tokens on, the cache from 2^35 / d rows, pbs_decode_attn from 2^26 rows of queries, 2^24 with a prefix or many pieces).
  * The other conventions above hold: host-validated, nothing allocated, no synchronisation, deterministic.
  */
 typedef struct { int64_t token, head; } pbs_strides;
@@ -391,8 +393,8 @@ typedef struct {
  * pbs_cache_read is the way back: row t of K, V [tokens, h_kv, d] of `dtype` becomes what slot slots[t] stands for
  * (the held value times its factor in fp32, rounded to dtype), zeros for a slot outside the cache.  K or V may be NULL
  * (then it is not read back); slots may repeat.
- * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, page, h_kv > 65535, more than 2^31 - 1 slots or
- * 2^31 - 256 rows), PBS_ERR_HIP.
+ * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, page, h_kv > 65535, more than 2^31 - 1 slots,
+ * 2^35 / d rows or more), PBS_ERR_HIP.
  */
 pbs_status pbs_cache_write(const pbs_cache *c, int32_t dtype, int32_t tokens, const void *K, const pbs_strides *k,
                            const void *V, const pbs_strides *v, const int32_t *slots, void *stream);

@@ -165,6 +165,9 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheArgs a, 
     store8(out + (int64_t)t * st.token + (int64_t)h * st.head + 8 * lane, x);
 }
 
+inline long long cache_groups(const CacheArgs &a) { return (((int64_t)a.rows << (a.d_log - 3)) + kCacheThreads - 1) / kCacheThreads; }
+inline dim3 cache_grid(const CacheArgs &a, int y) { return dim3((unsigned)cache_groups(a), y); }
+
 inline pbs_status cache_args(const pbs_cache *c, int32_t dtype, int32_t tokens, const int32_t *slots, CacheArgs &a)
 {
     const pbs_status st = check_cache(c);
@@ -180,12 +183,8 @@ inline pbs_status cache_args(const pbs_cache *c, int32_t dtype, int32_t tokens, 
     a.slots = c->pages * c->page;
     a.d_log = (unsigned)log2_of(c->d);
     a.slot = slots;
+    if (!fits_grid(cache_groups(a), kCacheThreads)) return PBS_ERR_UNSUPPORTED;
     return PBS_OK;
-}
-
-inline dim3 cache_grid(const CacheArgs &a, int y)
-{
-    return dim3((unsigned)((((int64_t)a.rows << (a.d_log - 3)) + kCacheThreads - 1) / kCacheThreads), y);
 }
 
 template <typename E>

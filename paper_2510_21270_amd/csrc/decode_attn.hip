@@ -713,7 +713,8 @@ struct DecodePlan {
     DecodeArgs a;
     int nt, p_nt;
     bool whole, join;
-    long long grid;                                        // workgroups of the own keys, 0: there are none
+    int join_rows;                                         // of a workgroup of the join
+    long long grid, join_grid;                             // workgroups of the own keys (0: there are none), of the join
     size_t bytes;                                          // of the workspace, and where in it:
     size_t part_o, part_ml, piece_o, piece_ml, pieces, line_k, line_v, line_kf, line_vf;
 };
@@ -777,6 +778,9 @@ inline pbs_status plan_decode(const pbs_decode_problem *p, const pbs_cache *c, D
     plan.grid = ((plan.whole ? units : a.max_len > 0 ? a.shares : 0) + kDecWaves - 1) / kDecWaves;
     a.shares = (int)(plan.whole ? 0 : plan.grid * kDecWaves);
     plan.join = !plan.whole && !(plan.grid == 0 && a.p_parts == 1 && plan.p_nt > 0);
+    plan.join_rows = a.p_parts > 0 || a.shares > 2 * (int64_t)units ? 1 : kDecWaves;
+    plan.join_grid = plan.join ? ((long long)a.n_seq * a.q_len * a.h_q + plan.join_rows - 1) / plan.join_rows : 0;
+    if (!fits_grid(plan.grid, kDecThreads) || !fits_grid(plan.join_grid, kDecThreads)) return PBS_ERR_UNSUPPORTED;
     const size_t all = plan.join ? (size_t)a.n_seq * a.q_len * a.h_q * (size_t)a.p_parts : 0;
     const size_t slots = plan.join && plan.grid ? (size_t)(units + a.shares) * a.slot_rows : 0;
     size_t at = 0;
@@ -819,10 +823,8 @@ pbs_status launch_decode(const DecodePlan &plan, hipStream_t s)
         st = a.q_len == 1 ? (plan.whole ? launch_own<DTYPE, D, false, true>(plan, s) : launch_own<DTYPE, D, false, false>(plan, s))
                           : (plan.whole ? launch_own<DTYPE, D, true, true>(plan, s) : launch_own<DTYPE, D, true, false>(plan, s));
     if (st != PBS_OK || !plan.join) return st;
-    const int64_t rows = (int64_t)a.n_seq * a.q_len * a.h_q;
-    if (a.p_parts > 0 || a.shares > 2 * (int64_t)a.n_seq * a.units)
-        return launch(decode_join_kernel<D, 1>, dim3((unsigned)rows), dim3(kDecThreads), 0, s, a, 16 * plan.nt);
-    return launch(decode_join_kernel<D, kDecWaves>, dim3((unsigned)((rows + kDecWaves - 1) / kDecWaves)), dim3(kDecThreads), 0, s, a, 16 * plan.nt);
+    return launch(plan.join_rows == 1 ? decode_join_kernel<D, 1> : decode_join_kernel<D, kDecWaves>, dim3((unsigned)plan.join_grid),
+                  dim3(kDecThreads), 0, s, a, 16 * plan.nt);
 }
 
 }  // namespace pbs

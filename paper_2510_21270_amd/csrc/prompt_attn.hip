@@ -184,7 +184,7 @@ extern "C" pbs_status pbs_prompt_attn(const pbs_prompt_problem *p, const void *Q
     const long long stride = p->k.token > p->v.token ? p->k.token : p->v.token;
     if (!rows_have_places(p->total_k, prompt::KS, stride * 2, p->d * 2)) return PBS_ERR_UNSUPPORTED;
     const long long grid = ((long long)p->total_q / tokens + p->n_seq) * p->h_kv;
-    if (grid > 0x7fffffffLL) return PBS_ERR_UNSUPPORTED;
+    if (!fits_grid(grid, 128)) return PBS_ERR_UNSUPPORTED;
     if (O == Q || (p->total_k > 0 && (O == K || O == V))) return PBS_ERR_SHAPE;              // rows may be formed a second time
 
     prompt::Args a;

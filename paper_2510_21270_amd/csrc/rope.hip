@@ -133,7 +133,9 @@ extern "C" pbs_status pbs_rope(const pbs_rope_problem *p, const double *freq, co
     a.in_place_k = K == Kout;
     if (p->h_q > 0 && a.in_place_q && (p->q.token != p->q_out.token || p->q.head != p->q_out.head)) return PBS_ERR_SHAPE;
     if (p->h_kv > 0 && a.in_place_k && (p->k.token != p->k_out.token || p->k.head != p->k_out.head)) return PBS_ERR_SHAPE;
-    const dim3 grid((unsigned)ceil_div(p->tokens, a.per_wg)), block(kRopeThreads);
+    const long long groups = ((long long)p->tokens + a.per_wg - 1) / a.per_wg;
+    if (!fits_grid(groups, kRopeThreads)) return PBS_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)groups), block(kRopeThreads);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (p->dtype == PBS_BF16)
         return launch(rope_kernel<bf16_t>, grid, block, 0, s, a, freq, positions, static_cast<const bf16_t *>(Q),

@@ -28,6 +28,9 @@ inline bool good_output(const void *x, const pbs_strides &s, long long tokens, l
     return s.token >= s.head ? s.head >= d && s.token >= s.head * heads : s.token >= d && s.head >= s.token * tokens;
 }
 
+// Whether `groups` workgroups of `threads` along x are one launch: a dispatch counts its threads in 32 bits.
+inline bool fits_grid(long long groups, int threads) { return groups * threads < 0x100000000ll; }
+
 inline pbs_status check_cache(const pbs_cache *c)
 {
     if (!c) return PBS_ERR_NULL;

@@ -51,3 +51,39 @@ def test_the_prefix_limits_rows_only_where_there_is_one(lib):
     assert lib.pbs_decode_workspace_bytes(ctypes.byref(p), ctypes.byref(c)) > 0
     p.prefix_len = 100
     assert lib.pbs_decode_workspace_bytes(ctypes.byref(p), ctypes.byref(c)) == 0 and _decode_call(lib, p, c, 4096, 4096) == 3
+
+
+# A dispatch holds fewer than 2^32 threads along x; larger calls are refused before anything is enqueued.
+def test_rotation_of_more_tokens_than_a_grid_holds(lib):
+    p = b.pbs_rope_problem(tokens=2 ** 24, h_q=32, h_kv=8, d=128, rot=128, layout=0, dtype=1, magnitude=1.0, flags=0)
+    p.q = p.q_out = b.pbs_strides(32 * 128, 128)
+    p.k = p.k_out = b.pbs_strides(8 * 128, 128)
+    assert lib.pbs_rope(ctypes.byref(p), _at(4096), _at(4096), _at(4096), _at(4096), _at(1 << 20), _at(1 << 21), None) == 3
+
+
+@pytest.mark.parametrize("d,tokens", [(128, 2 ** 25), (64, 2 ** 26)])
+def test_more_cache_rows_than_a_grid_holds(lib, d, tokens):
+    c, s = _cache(d=d, h_kv=8), b.pbs_strides(8 * d, d)
+    assert lib.pbs_cache_write(ctypes.byref(c), 1, tokens, _at(4096), ctypes.byref(s), _at(4096), ctypes.byref(s), _at(4096), None) == 3
+    assert lib.pbs_cache_read(ctypes.byref(c), 1, tokens, _at(4096), _at(4096), ctypes.byref(s), _at(4096), ctypes.byref(s), None) == 3
+
+
+@pytest.mark.parametrize("n_seq,q_len,h_q,h_kv,prefix,max_len", [(65535, 16, 32, 4, 100, 0),           # the join of a prefix's parts
+                                                                 (65535, 16, 2048, 2048, 0, 16),       # own keys, a wave to a unit
+                                                                 (65535, 16, 66, 2, 0, 8000)])         # the join of their pieces
+def test_more_rows_of_new_tokens_than_a_grid_holds(lib, n_seq, q_len, h_q, h_kv, prefix, max_len):
+    c = _cache(h_kv=h_kv)
+    p = _decode(n_seq=n_seq, q_len=q_len, h_q=h_q, max_pages=500, max_len=max_len, prefix_len=prefix)
+    p.q = p.o = b.pbs_strides(h_q * 64, 64)
+    assert _decode_call(lib, p, c, 4096, 1 << 20) == 3
+    assert lib.pbs_decode_workspace_bytes(ctypes.byref(p), ctypes.byref(c)) == 0
+
+
+def test_more_prompt_tiles_than_a_grid_holds(lib):
+    p = b.pbs_prompt_problem(n_seq=1, total_q=2 ** 26, total_k=64, h_q=16, h_kv=16, d=64, dtype=1, scale=0.0, flags=1)
+    p.q = p.k = p.v = p.o = b.pbs_strides(16 * 64, 64)
+    grid = p.total_q // 128 * 16
+    assert grid * 128 < 2 ** 32                            # 2^30 rows: the largest number of tiles stays below
+    p = b.pbs_prompt_problem(n_seq=2 ** 22, total_q=2 ** 22, total_k=64, h_q=16, h_kv=16, d=64, dtype=1, scale=0.0, flags=1)
+    p.q = p.k = p.v = p.o = b.pbs_strides(16 * 64, 64)
+    assert lib.pbs_prompt_attn(ctypes.byref(p), _at(4096), _at(8192), _at(8192), _at(4096), _at(4096), _at(1 << 20), None, None) == 3
