@@ -571,8 +571,10 @@ def decode_attn(cache, Q, page_table, lens, max_len=None, prefix_pages=None, pre
     p = _DECODE(n, q_len, h_q, max_pages, max_len, prefix_len, _DTYPE_CODES.get(Q.dtype, -1), scale, *_token_strides(what, Q),
                 *_token_strides(what, O))
     need = lib.pbs_decode_workspace_bytes(p, cache.c)
-    if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
+    elif not ws.is_contiguous():
+        _refuse(what, "ws has to be contiguous")
     _same_device(what, dev, Q, O, page_table, lens, prefix_pages, lse, ws)
     _launch(what, dev, lib.pbs_decode_attn, p, cache.c, Q.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
             prefix_pages.data_ptr() if prefix_pages is not None else None, O.data_ptr(),

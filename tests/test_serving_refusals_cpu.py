@@ -87,3 +87,17 @@ def test_more_prompt_tiles_than_a_grid_holds(lib):
     p = b.pbs_prompt_problem(n_seq=2 ** 22, total_q=2 ** 22, total_k=64, h_q=16, h_kv=16, d=64, dtype=1, scale=0.0, flags=1)
     p.q = p.k = p.v = p.o = b.pbs_strides(16 * 64, 64)
     assert lib.pbs_prompt_attn(ctypes.byref(p), _at(4096), _at(8192), _at(8192), _at(4096), _at(4096), _at(1 << 20), None, None) == 3
+
+
+def test_a_workspace_that_is_a_strided_view_is_refused(monkeypatch):
+    # the kernels write consecutive bytes: every second byte of a buffer would take them over the others
+    import torch
+    c = b.Cache.__new__(b.Cache)
+    c.dev, c.d, c.page, c.c = 0, 64, 16, b._CACHE(8, 16, 2, 64, 1, 4096, 4096, 0, 0)
+    monkeypatch.setattr(b, "_same_device", lambda *a: None)
+    monkeypatch.setattr(b, "_launch", lambda *a: None)
+    Q, table, lens = torch.zeros(2, 1, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 30, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    buf = torch.zeros(1 << 22, dtype=torch.uint8)
+    b.decode_attn(c, Q, table, lens, ws=buf)
+    with pytest.raises(b.PbsError, match="ws has to be contiguous"):
+        b.decode_attn(c, Q, table, lens, ws=buf[::2])
