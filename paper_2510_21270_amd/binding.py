@@ -370,6 +370,13 @@ def _refuse(what, why):
     raise PbsError("%s: %s" % (what, why))
 
 
+def _packed(what, pack, *numbers):
+    try:
+        return pack(*numbers)
+    except (struct.error, OverflowError) as e:
+        raise PbsError("%s: a number that its structure cannot hold (%s)" % (what, e)) from None
+
+
 def _same_device(what, dev, *tensors):
     """All tensors (None: not given) lie on GPU `dev`."""
     if dev < 0:
@@ -456,9 +463,9 @@ def rope(Q, K, positions, freq, layout="half", magnitude=1.0, transpose=False, Q
         heads[k] = t.shape[1]
         strides += _rows(what, t) + _rows(what, out)
         places.append((t.data_ptr(), out.data_ptr()))
-    p = _ROPE(tokens, heads[0], heads[1], d, 2 * freq.shape[0], ROPE_LAYOUTS[layout], _DTYPE_CODES.get(dt, -1), magnitude,
-              ROPE_TRANSPOSE if transpose else 0, strides[0], strides[1], strides[4], strides[5], strides[2], strides[3],
-              strides[6], strides[7])
+    p = _packed(what, _ROPE, tokens, heads[0], heads[1], d, 2 * freq.shape[0], ROPE_LAYOUTS[layout], _DTYPE_CODES.get(dt, -1),
+                magnitude, ROPE_TRANSPOSE if transpose else 0, strides[0], strides[1], strides[4], strides[5], strides[2],
+                strides[3], strides[6], strides[7])
     _launch(what, dev, (_lib or load_library()).pbs_rope, p, freq.data_ptr(), positions.data_ptr(), places[0][0], places[1][0],
             places[0][1], places[1][1])
     return Qout, Kout
@@ -568,8 +575,8 @@ def decode_attn(cache, Q, page_table, lens, max_len=None, prefix_pages=None, pre
             lse = torch.empty((n, q_len, h_q), dtype=torch.float32, device=Q.device)
     elif lse.dtype != torch.float32 or lse.shape != (n, q_len, h_q) or not lse.is_contiguous():
         _refuse(what, "lse has to be contiguous float32 [n_seq, q_len, h_q]")
-    p = _DECODE(n, q_len, h_q, max_pages, max_len, prefix_len, _DTYPE_CODES.get(Q.dtype, -1), scale, *_token_strides(what, Q),
-                *_token_strides(what, O))
+    p = _packed(what, _DECODE, n, q_len, h_q, max_pages, max_len, prefix_len, _DTYPE_CODES.get(Q.dtype, -1), scale,
+                *_token_strides(what, Q), *_token_strides(what, O))
     need = lib.pbs_decode_workspace_bytes(p, cache.c)
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
@@ -614,7 +621,7 @@ def prompt_attn(Q, K, V, cu_q, cu_k=None, causal=True, scale=0.0, O=None, lse=No
     elif lse.dtype != torch.float32 or lse.shape != (total, h_q) or not lse.is_contiguous():
         _refuse(what, "lse has to be contiguous float32 [total_q, h_q]")
     _same_device(what, dev, K, V, cu_q, cu_k, O, lse)
-    p = _PROMPT(n - 1, total, total_k, h_q, h_kv, d, _DTYPE_CODES.get(dt, -1), scale, PROMPT_CAUSAL if causal else 0,
+    p = _packed(what, _PROMPT, n - 1, total, total_k, h_q, h_kv, d, _DTYPE_CODES.get(dt, -1), scale, PROMPT_CAUSAL if causal else 0,
                 *_rows(what, Q), *_rows(what, K), *_rows(what, V), *_rows(what, O))
     _launch(what, dev, (_lib or load_library()).pbs_prompt_attn, p, Q.data_ptr(), K.data_ptr(), V.data_ptr(), cu_q.data_ptr(),
             cu_k.data_ptr(), O.data_ptr(), lse.data_ptr() if lse is not None else None)
@@ -691,8 +698,8 @@ class DecodeStep:
         self.prefix_pages, self.prefix_len = prefix_pages, prefix_len
         self.max_len = max_pages * cache.page if max_len is None else max_len
         self.O = torch.empty((n_seq, q_len, h_q, cache.d), dtype=torch.bfloat16, device=cache.K.device)
-        p = _DECODE(n_seq, q_len, h_q, max_pages, self.max_len, prefix_len, PBS_BF16, scale, h_q * cache.d, cache.d,
-                    h_q * cache.d, cache.d)
+        p = _packed("pbs_decode_attn", _DECODE, n_seq, q_len, h_q, max_pages, self.max_len, prefix_len, PBS_BF16, scale,
+                    h_q * cache.d, cache.d, h_q * cache.d, cache.d)
         need = load_library().pbs_decode_workspace_bytes(p, cache.c)
         self.ws = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.K.device)
 

@@ -101,3 +101,16 @@ def test_a_workspace_that_is_a_strided_view_is_refused(monkeypatch):
     b.decode_attn(c, Q, table, lens, ws=buf)
     with pytest.raises(b.PbsError, match="ws has to be contiguous"):
         b.decode_attn(c, Q, table, lens, ws=buf[::2])
+
+
+def test_numbers_that_the_structures_cannot_hold_are_refused(monkeypatch):
+    import torch
+    monkeypatch.setattr(b, "_same_device", lambda *a: None)
+    monkeypatch.setattr(b, "_launch", lambda *a: None)
+    c = b.Cache.__new__(b.Cache)
+    c.dev, c.d, c.page, c.c = 0, 64, 16, b._CACHE(8, 16, 2, 64, 1, 4096, 4096, 0, 0)
+    Q, table, lens = torch.zeros(2, 1, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 30, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    pages = torch.zeros(30, dtype=torch.int32)
+    for kw in (dict(max_len=1 << 31), dict(max_len=1 << 70), dict(prefix_len=-(1 << 40))):
+        with pytest.raises(b.PbsError, match="pbs_decode_attn"):
+            b.decode_attn(c, Q, table, lens, prefix_pages=pages, **kw)
