@@ -418,7 +418,8 @@ pbs_status pbs_cache_read(const pbs_cache *c, int32_t dtype, int32_t tokens, con
  *   lse      [n_seq * q_len, h_q] float32 or NULL: log-sum-exp of the logits that each query sees.
  *   ws       pbs_decode_workspace_bytes(p, c) bytes, 256-byte aligned (0: may be NULL); need not be initialised, means
  *            nothing afterwards.  Calls that may overlap in time need one each.
- * Probabilities enter the second product in bf16, everything else is fp32.
+ * Probabilities, with a value row's factor in them, enter the second product as two terms in bf16 (2^-16 of each is lost at most), against
+ * a prefix that is read for 128 rows at a time as one (2^-8 at most); everything else is fp32.
  * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE (max_len or prefix_len negative, misaligned, a scale that is negative or not
  * finite), PBS_ERR_UNSUPPORTED (q_len > 16, n_seq > 65535, n_seq * q_len * h_q or n_seq * max_pages > 2^31 - 1,
  * max_len > 2^27, prefix_len > 2^25, a grid that is too large, dtype), PBS_ERR_WORKSPACE, PBS_ERR_HIP.
@@ -444,7 +445,7 @@ pbs_status pbs_decode_attn(const pbs_decode_problem *p, const pbs_cache *c, cons
  * key, or whose logits are all -inf, gets a zero row and lse = -inf.  Rows of O and lse that belong to no sequence stay as they were.
  *   Q, O [total_q, h_q, d], K, V [total_k, h_kv, d], bf16; h_q % h_kv == 0, h_q / h_kv <= 128; lse [total_q, h_q] float32 or NULL.
  *   O may not overlap Q, K or V (PBS_ERR_SHAPE where it starts at one of them).
- * Probabilities enter the second product in bf16, everything else is fp32.
+ * Probabilities enter the second product rounded to bf16 (off by 2^-8 of each at most), everything else is fp32.
  * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE, PBS_ERR_UNSUPPORTED (dtype, d, h_q / h_kv > 128, rows beyond 2^31 - 1, a grid that is
  * too large, K or V of one head spanning 2 GiB or more), PBS_ERR_HIP.
  */

@@ -8,7 +8,9 @@
 // {4g + i} of both tiles, so it loads these eight rows of V, 8 (d = 64: 4) features of each, and turns the little square with
 // byte moves.  Nothing goes through LDS: each wave streams its own keys from memory into registers, a tile of 32 keys ahead
 // of the one it multiplies.  8-bit values become bf16 exactly; a key's factor is applied to its logit, a value row's
-// to its probability.
+// to its probability.  A probability enters the product as two terms in bf16 (its rounding alone would be off by 2^-8 of it, as much as O's
+// own): the matrix units wait for the keys.  Measured, one term / two: 8 sequences of 131072 keys in bf16 719 / 717 us, 64 of 7 .. 16000
+// in e4m3 58.5 / 58.6, in int8 60.0 / 60.5, of 64 features in int8 38.2 / 39.6, 2 of 9000 in int8 with 8 new tokens 28.3 / 29.2.
 //
 // The bytes of the cache bound it, and a batch's lengths differ by orders of magnitude, known to the device alone.  The tiles of
 // all (sequence, kv head) units lie one behind the other in thought, and every wave takes an equal share of that row of
@@ -102,7 +104,9 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t pair)
 // One tile of 32 keys, the first of them key0.  Keys below sees[nt] are visible to the lane's query, keys below `all` to every
 // query of the call, keys at or above `none` to no query.  SEVERAL: sees differs between queries; what is not finite in rows
 // that some of them see is left out (a hidden row's weight is zero, but 0 * inf is NaN), and `dropped` says so.
-template <int DTYPE, int D, int NT, bool SEVERAL>
+// A weight enters the second product as two terms in bf16, itself rounded and what that leaves, 2^-16 of it at most being lost.  ODD: the
+// values may not be finite; the rest, which has any sign or is zero, takes the finite ones only.
+template <int DTYPE, int D, int NT, bool SEVERAL, bool ODD>
 __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile32<DTYPE, D> &t, const bf16x8 (&q)[D / 32][NT],
                                               const int (&sees)[NT], int key0, int all, int none, float c2, int g, bool &dropped)
 {
@@ -124,7 +128,7 @@ __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile
                 s[u][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, q[x][nt], x == 0 ? floatx4{0} : s[u][nt], 0, 0, 0);
         }
     const bool masked = key0 + kTileKeys > all || !t.ok[0] || !t.ok[1];      // uniform
-    bf16x8 p[NT];
+    bf16x8 p[NT], rest[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         float y[8], top = -INFINITY;
@@ -150,6 +154,7 @@ __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile
                 w = masked && y[e] == -INFINITY ? 0.0f : w * f;   // the factor of a hidden row may be NaN
             }
             p[nt][e] = (bf16_t)w;
+            rest[nt][e] = (bf16_t)(w - (float)p[nt][e]);
         }
         st.l[nt] = st.l[nt] * alpha + sum;
         if (__any(alpha != 1.0f)) {
@@ -198,8 +203,23 @@ __device__ __forceinline__ void multiply_tile(DecodeState<D, NT> &st, const Tile
     for (int j = 0; j < NJ; ++j) {
         const bf16x8 va = __builtin_bit_cast(bf16x8, turned(j));
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
             st.o[j][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p[nt], st.o[j][nt], 0, 0, 0);
+            if (!ODD) st.o[j][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, rest[nt], st.o[j][nt], 0, 0, 0);
+        }
+    }
+    if constexpr (ODD) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int x = 0; x < NJ / 2; ++x) w[e][x] = finite_part(w[e][x]);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const bf16x8 va = __builtin_bit_cast(bf16x8, turned(j));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+                st.o[j][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, rest[nt], st.o[j][nt], 0, 0, 0);
+        }
     }
 }
 
@@ -233,6 +253,15 @@ __device__ __forceinline__ void walk_keys(DecodeState<D, NT> &st, const DecodeAr
     hold(0);
     bf16x8 q[D / 32][NT];
     int sees[NT];
+    auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            st.m[nt] = -INFINITY;
+            st.l[nt] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) st.o[j][nt] = floatx4{0};
+        }
+    };
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int rc = min(row0 + 16 * nt + c, rows - 1), t = rc / a.r;
@@ -241,17 +270,14 @@ __device__ __forceinline__ void walk_keys(DecodeState<D, NT> &st, const DecodeAr
         for (int x = 0; x < D / 32; ++x)
             q[x][nt] = *reinterpret_cast<const bf16x8 *>(src + (DTYPE == PBS_BF16 ? 32 * x + 8 * g : 64 * (x >> 1) + 16 * g + 8 * (x & 1)));
         sees[nt] = OWN ? len - a.q_len + t + 1 : len;
-        st.m[nt] = -INFINITY;
-        st.l[nt] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) st.o[j][nt] = floatx4{0};
     }
+    clear();
     const int all = OWN ? len - a.q_len + 1 : len;
 
     Tile32<DTYPE, D> ta, tb;
     bool dropped = false;
     auto use = [&](const Tile32<DTYPE, D> &t, int it) __attribute__((always_inline)) {
-        multiply_tile<DTYPE, D, NT, SEVERAL>(st, t, q, sees, (first + STEP * it) * kTileKeys, all, len, a.c2, g, dropped);
+        multiply_tile<DTYPE, D, NT, SEVERAL, false>(st, t, q, sees, (first + STEP * it) * kTileKeys, all, len, a.c2, g, dropped);
     };
     if (mine > 0) fetch(ta, 0);
     for (int it = 0; it < mine; it += 2) {
@@ -263,6 +289,24 @@ __device__ __forceinline__ void walk_keys(DecodeState<D, NT> &st, const DecodeAr
                 fetch(ta, it + 2);
             }
             use(tb, it + 1);
+        }
+    }
+    if constexpr (DTYPE != PBS_I8) {                       // (int8 values are finite)
+        // values that are not finite show in O^T: such a wave goes over its keys again
+        float zero = 0.0f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(st.o[j][nt][i], 0.0f, zero);
+        if (__builtin_expect(__any(zero != 0.0f), 0)) {
+            clear();
+            for (int it = 0; it < mine; ++it) {
+                if ((it & (kHeldTiles - 1)) == 0) hold(it);
+                fetch(ta, it);
+                multiply_tile<DTYPE, D, NT, SEVERAL, true>(st, ta, q, sees, (first + STEP * it) * kTileKeys, all, len, a.c2, g, dropped);
+            }
         }
     }
     if constexpr (SEVERAL && DTYPE != PBS_I8) {
