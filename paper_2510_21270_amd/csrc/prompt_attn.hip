@@ -156,7 +156,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             whole_tile<D>(st, sg0, off, q, sees, t * KS, 3, a.c2, h);
         }
         __syncthreads();
-        const bool bad = store_rows<D>(a, pl, st, sees, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));
+        store_rows<D>(a, pl, st, sees, kv, t0, rows, wave, lane, reinterpret_cast<unsigned char *>(wave == 0 ? &sg0 : &sg1));
     }
 }
 
