@@ -417,7 +417,10 @@ pbs_status pbs_cache_read(const pbs_cache *c, int32_t dtype, int32_t tokens, con
  *            128 rows (query, head of its group) of the whole batch at a time, not once per sequence.
  *   lse      [n_seq * q_len, h_q] float32 or NULL: log-sum-exp of the logits that each query sees.
  *   ws       pbs_decode_workspace_bytes(p, c) bytes, 256-byte aligned (0: may be NULL); need not be initialised, means
- *            nothing afterwards.  Calls that may overlap in time need one each.
+ *            nothing afterwards.  Calls that may overlap in time need one each.  Behind a prefix it holds d + 2 floats for every
+ *            row of Q and part of the prefix (1024 keys at most where it is read for 128 rows at a time: 256 rows of 32 heads of 128
+ *            behind 131072 keys take 545 MB), and, there and in 8 bits, the prefix in bf16; without one d + 2 floats for the
+ *            rows, 32 at most, of every (sequence, kv head) and of 2048 pieces (4096 sequences of 8 kv heads 73 MB).
  * Probabilities, with a value row's factor in them, enter the second product as two terms in bf16 (2^-16 of each is lost at most), against
  * a prefix that is read for 128 rows at a time as one (2^-8 at most); everything else is fp32.
  * Errors: PBS_ERR_NULL, PBS_ERR_SHAPE (max_len or prefix_len negative, misaligned, a scale that is negative or not

@@ -17,8 +17,8 @@
 // tiles: the end of one unit, a few whole ones, the start of the next.  A piece of a unit leaves O^T, m and l in the
 // workspace and a second launch joins the pieces; a unit that lies in one share whole is stored at once.  The prefix is
 // cut into parts of its keys, and its rows are the queries of the whole batch: its keys are read for 16 or 32 rows at a time (or
-// 128, prefix_attn.hip).  Measured, 32 query heads on 8 of 128, replayed: 8 sequences of 131072 keys in bf16 710 us (6.0 TB/s), 64 of
-// 7 .. 16000 in e4m3 60 us (4.9 TB/s), one of 1000 keys 9.3 us (two launches, latency).
+// 128, prefix_attn.hip).  Measured, 32 query heads on 8 of 128, replayed: 8 sequences of 131072 keys in bf16 717 us (6.0 TB/s), 64 of
+// 7 .. 16000 in e4m3 59 us (5.0 TB/s), one of 1000 keys 9.4 us (two launches, latency).
 #include <type_traits>
 
 #include "decode.h"
@@ -741,10 +741,10 @@ inline int part_keys(int64_t units, int64_t keys)
 
 // Whether decode_prefix_kernel, 16 or 32 rows to a workgroup, reads the prefix, or, from more rows on, the kernel of
 // prefix_attn.hip, 128 rows to a workgroup.  The latter multiplies faster but starts and ends slower, and it wants 8-bit values
-// written out as bf16, which costs as much as four passes of the former over them.  Measured, whole call, us, this kernel / that:
-// bf16, 8 kv heads, 8000 keys: 64 rows 28 / 34, 128 rows 35 / 37, 160 rows 39 / 36, 256 rows 49 / 40; 2000 keys, 256 rows 28 / 35;
-// 32000 keys, 96 rows 62 / 48.  e4m3: 8000 keys, 128 rows 34 / 49, 256 rows 50 / 51; 32000 keys, 128 rows 77 / 84, 256 rows
-// 139 / 100.
+// written out as bf16, which costs as much as four passes of the former over them.  Measured, replayed, us, this kernel / that, 8 kv
+// heads: bf16, 8000 keys: 64 rows 26 / 28, 128 rows 34 / 34, 160 rows 40 / 33, 256 rows 51 / 38; 2000 keys, 256 rows 28 / 33;
+// 32000 keys, 96 rows 65 / 43.  e4m3: 8000 keys, 128 rows 34 / 44, 256 rows 52 / 48; 32000 keys, 128 rows 81 / 79, 256 rows
+// 149 / 94.  Where they are equal it is the former, whose probabilities have two terms.
 inline int prefix_tiles(int64_t rows, int h_kv, int64_t keys, int dtype)
 {
     if (rows <= 16) return 1;

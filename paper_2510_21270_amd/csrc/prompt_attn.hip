@@ -2,8 +2,8 @@
 //
 // The rows of a workgroup are (token, head of the group): all query heads of a kv head share every key tile, 128 rows span few
 // tokens, so that little is multiplied above the diagonal and short prompts fill their tiles.  32 heads on 8 of 128: 16384 tokens
-// 1.72 ms (1.28 PFLOP/s, matrix units 80 % busy), 16 prompts of 33 .. 2048 tokens 110 us (0.74), of which a workgroup's start and end
-// are about 7 of 20 us; 4 prompts of 1 .. 200 tokens 13.2 us.
+// 1.70 ms where calls leave the chip pauses (1.29 PFLOP/s), 1.77 one behind the other (1.24, matrix units 80 % busy), 16 prompts of 33 ..
+// 2048 tokens 103 to 110 us (0.74), of which a workgroup's start and end are about 7 of 20 us; 4 prompts of 1 .. 200 tokens 13.2 us.
 #include "key_pipeline.h"
 
 namespace pbs {
