@@ -82,6 +82,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
             Rows<D, true> s;
             const int64_t first = (int64_t)kv * a.p_room + begin;
             s.size = count * D * 2;
+            s.tiles = tiles;
             s.tile_bytes = KS * D * 2;
             s.factors_size = min(a.p_chunk, a.p_room - begin) * 4;
             s.rows = __builtin_amdgcn_make_buffer_rsrc((wave == 0 ? a.line_k : a.line_v) + first * D, 0, s.size, 0x00020000);
