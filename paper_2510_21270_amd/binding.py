@@ -877,6 +877,8 @@ class DecodeStep:
     With a `rule` attention is decode_attn_rule (without a prefix); with `marks` of the cache the new rows are marked with their
     positions and weight 0, the keys' positions count, and what every key receives is added to its weight."""
 
+    marks = rule = None
+
     def __init__(self, cache, n_seq, h_q, max_pages, freq, q_len=1, max_len=None, layout="half", magnitude=1.0,
                  prefix_pages=None, prefix_len=0, scale=0.0, rule=None, marks=None):
         self.cache, self.freq, self.layout, self.magnitude, self.scale = cache, freq, layout, magnitude, scale
@@ -917,13 +919,20 @@ class DecodeStep:
         return cache_evict(self.marks, page_table, lens, budget, sinks, recent, self.max_len, new_lens=lens)
 
     def capture(self, *args):
-        """Record a step into a HIP graph that reads these very tensors (refill them in place, then replay()).  Q and K are
-        turned by every run, the ones before the recording among them."""
+        """Record a step into a HIP graph that reads these very tensors (refill them in place, then replay()).  The run ahead of the
+        recording turns Q and K and writes and marks the new rows, as every run does; the marks' weights it leaves as they are: only
+        replays add to them."""
         with torch.cuda.device(self.cache.K.device):
             side = torch.cuda.Stream()
             side.wait_stream(torch.cuda.current_stream())
+            marks = self.marks
             with torch.cuda.stream(side):
-                self.run(*args)
+                try:
+                    if marks is not None and marks.weight is not None:         # weights of its own, for the same kernels
+                        self.marks = CacheMarks(self.cache, torch.zeros_like(marks.weight), marks.position)
+                    self.run(*args)
+                finally:
+                    self.marks = marks
             torch.cuda.current_stream().wait_stream(side)
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph):
