@@ -831,13 +831,21 @@ class Pipeline:
         """With a `cache` the keys and values also go into its slots [batch, n], for the decode steps behind the prompt; with `marks`
         of it the rows get their positions [batch, n] and, as their first weights, the scores of Eq. 4."""
         p = self.p
+        # all refusals of the rows and their marks come before the first row is written
+        if cache is not None and (slots is None or slots.shape != (p.batch, p.n)):
+            _refuse("pbs_cache_write", "a cache needs slots [batch, n]")
+        if marks is not None:
+            what = "pbs_cache_mark"
+            if cache is None or marks.cache is not cache or (positions is not None and positions.shape != slots.shape):
+                _refuse(what, "marks need the cache that they belong to, its slots and positions [batch, n]")
+            if marks.position is not None and positions is None:
+                _refuse(what, "positions are missing")
+            for b in range(p.batch if positions is not None else 0):
+                _ints(what, positions[b], "positions", p.n)
+            _same_device(what, cache.dev, slots, positions)
         if cache is not None:
-            if slots is None or slots.shape != (p.batch, p.n):
-                _refuse("pbs_cache_write", "a cache needs slots [batch, n]")
             for b in range(p.batch):
                 cache_write(cache, K[b].transpose(0, 1), V[b].transpose(0, 1), slots[b])
-        if marks is not None and (cache is None or marks.cache is not cache or (positions is not None and positions.shape != slots.shape)):
-            _refuse("pbs_cache_mark", "marks need the cache that they belong to, its slots and positions [batch, n]")
         key_scores(p, Q, K, self.scores, self.ws1)
         if marks is not None:
             for b in range(p.batch):
