@@ -537,7 +537,9 @@ pbs_status pbs_cache_mark(const pbs_cache *c, const pbs_cache_marks *marks, int3
 /*
  * Eviction: every (sequence, kv head) keeps at most `budget` of its own keys, each head its own.  In this order: those that are
  * protected (position below `sinks`, or among the positions newest - recent + 1 .. newest, newest being the head's largest), those with
- * larger weights (a weight that is negative or NaN counts as 0), those at lower places.  new_lens[i] = min(lens[i], budget); of
+ * larger weights (a weight that is negative or NaN counts as 0), those at lower places.  Among protected ones the weights do not count:
+ * where more of them than may stay are there (positions below 0, the same position more than once, rows that cannot be moved, see
+ * below), those at the lowest places do.  new_lens[i] = min(lens[i], budget); of
  * the places below it those whose rows do not stay receive, in ascending order, the rows that stay from the places behind, in
  * ascending order: K, V, factors, weight and position.  Every other row stays as it was, the ones behind new_lens[i] among them; the pages
  * behind the last key of all heads can be given away.
