@@ -487,7 +487,8 @@ typedef struct {
  *   prefix   [n_seq] int32, device memory, or NULL: keys at positions below prefix[i] are seen by every query of sequence i, whatever
  *            their order and the window (a prompt whose first part attends to itself in both directions).
  * A query that sees no key gets a zero row and lse = -inf.  A workgroup reads the keys between the first and the last that some of its
- * rows see, without those between prefix or sinks and the window.  Everything else as for pbs_prompt_attn.
+ * rows see, without those between prefix or sinks and the window.  Everything else as for pbs_prompt_attn, probabilities in bf16 in the
+ * second product among it.
  */
 pbs_status pbs_prompt_attn_rule(const pbs_prompt_problem *p, const pbs_score_rule *rule, const void *Q, const void *K,
                                 const void *V, const int32_t *cu_q, const int32_t *cu_k, const int32_t *prefix, void *O,
@@ -496,7 +497,9 @@ pbs_status pbs_prompt_attn_rule(const pbs_prompt_problem *p, const pbs_score_rul
 /*
  * What a cache's rows are marked with: the attention that a row has received so far, and its token's position, for every
  * row [pages, h_kv, page] of the cache; device memory, 16-byte aligned, caller-owned.  An eviction moves rows (of each kv head others),
- * so that a key's place in its sequence is no longer its position.
+ * so that a key's place in its sequence is no longer its position.  A call of pbs_decode_attn_rule adds q_len * h_q / h_kv in all to the
+ * keys of a (sequence, kv head).  What pbs_cache_mark writes is on the caller's scale: the scores of pbs_key_scores, means over a block of
+ * queries, sum up to 1 for a kv head, so that one token of four heads to a kv head outweighs them four times; multiply them for more.
  */
 typedef struct {
     float *weight;

@@ -829,7 +829,8 @@ class Pipeline:
 
     def run(self, Q, K, V, qidx=None, cache=None, slots=None, marks=None, positions=None):
         """With a `cache` the keys and values also go into its slots [batch, n], for the decode steps behind the prompt; with `marks`
-        of it the rows get their positions [batch, n] and, as their first weights, the scores of Eq. 4."""
+        of it the rows get their positions [batch, n] and, as their first weights, the scores of Eq. 4, which sum up to 1 for a kv head (a
+        decode step adds q_len * h_q / h_kv; cache_mark with self.scores[b].T times a factor gives them another scale)."""
         p = self.p
         # all refusals of the rows and their marks come before the first row is written
         if cache is not None and (slots is None or slots.shape != (p.batch, p.n)):
@@ -921,7 +922,8 @@ class DecodeStep:
                            self.O, ws=self.ws)
 
     def evict(self, page_table, lens, budget, sinks=0, recent=0):
-        """Between two steps: at most `budget` keys of every sequence and kv head stay (cache_evict), lens is made that in place."""
+        """Between two steps: at most `budget` keys of every sequence and kv head stay (cache_evict), lens is made that in place.  The
+        bound on lens is the step's max_len; where the lengths are known to be far below it, cache_evict with theirs is faster."""
         if self.marks is None:
             _refuse("pbs_cache_evict", "a step without marks")
         return cache_evict(self.marks, page_table, lens, budget, sinks, recent, self.max_len, new_lens=lens)

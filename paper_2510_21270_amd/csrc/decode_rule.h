@@ -39,7 +39,7 @@ struct FormArgs : RuleArgs {
 
 // With positions a window may hide most tiles, and which ones is not known.  Where a wave may have many (by max_len), those that have
 // more than kFewTiles look at the positions of 32 tiles before they bring any, and a wave's tiles lie apart, as those that are seen
-// lie together.  Measured, replayed, with weights, one new token, 32 / 8 heads, bf16: 8 sequences of 131072 keys, a window of 4096, 955 -> 97 us
+// lie together.  Measured, a graph of one call, with weights, one new token, 32 / 8 heads, bf16: 8 sequences of 131072 keys, a window of 4096, 955 -> 97 us
 // (with neighbouring tiles to a wave 234), 8 of 16384 (16 tiles to a wave) 151 -> 68, and where the window hides nothing 151 / 151; 32 of 200 ..
 // 4097 keys, 3 new tokens, 28 / 4 heads, in int8 (16 tiles, each with two of rows) where every tile has a key that is seen 77 -> 80.
 constexpr int kFewTiles = 8, kManyTiles = 12;              // (the latter for 16 rows)
@@ -54,7 +54,8 @@ __device__ __forceinline__ Listed listed_tiles(const RuleArgs &a, int len)
     return {head, max(first - head, 0), 0};
 }
 
-// Lanes x and 32 + x hold the position of key x: one register to a tile.
+// Lanes x and 32 + x hold the position of key x: one register to a tile.  (The compiler has page and place of both halves, which a lane picks
+// by its number, in LDS: 12 to 16 KB in every form that may ask for positions.)
 template <int DTYPE, int D>
 struct RuleTile : Tile32<DTYPE, D> {
     int kp;

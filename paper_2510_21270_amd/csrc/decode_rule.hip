@@ -120,7 +120,7 @@ __device__ __forceinline__ void weigh_keys(const RuleArgs &a, int rows_of_unit, 
 }
 
 // The join's workgroups, `joins` of them (none where nothing is joined), and those of the weights: neither waits for the other.
-// What is left of a launch between them: 32 sequences of 200 .. 4097 keys, 3 new tokens, 28 / 4 heads, in int8, 82 -> 75 us; 64 of 7 .. 16000
+// What is left of a launch between them, graphs of one call: 32 sequences of 200 .. 4097 keys, 3 new tokens, 28 / 4 heads, in int8, 82 -> 75 us; 64 of 7 .. 16000
 // keys in e4m3 92 -> 90 (1024 keys to a workgroup, twice as many that form every lse, 94); 8 of 131072 the same.
 template <int D, int ROWS>
 __global__ __launch_bounds__(kDecThreads) void join_weigh_kernel(RuleArgs a, int rows_of_unit, unsigned joins, int chunks)

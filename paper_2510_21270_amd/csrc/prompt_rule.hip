@@ -14,11 +14,17 @@
 // tiles come newest first, where a bias leaves the largest scores.  Under a cap alone no reference is needed: scores are within
 // 2^+-80, and 32 bits hold their sums.  Values that are not finite (a hidden key's weight is zero, but 0 * inf is NaN) and sums that
 // came too near to the ends of the range show when the rows are stored; such a workgroup goes over its keys again, with a
-// reference and what is not finite counted apart.
+// reference and what is not finite counted apart.  With heads of 128 that pass holds up to 18 values of a lane in scratch memory; the loop
+// itself has all of its own in registers.
+//
+// Probabilities enter the second product as one term in bf16 (off by 2^-8 of each at most), while l sums them as they are.  A second term, what
+// the rounding leaves, takes O from 1.9 .. 2.4e-3 off the 64-bit form (rows' norms) to 1.6e-3, which is O's own rounding, but half as many
+// matrix instructions again have no slots: 16384 tokens under a cap 2420 -> 3190 us, 16 prompts of 33 .. 2048 under a window 89 -> 109,
+// 6 with a bias and prefixes 39 -> 47, 4 of 1 .. 200 11.1 -> 11.9.
 //
 // Issue slots bound the long prompts, starts and ends of workgroups the short ones.  Measured, us, 32 / 8 heads of 128: 16384 tokens under a cap
-// of 50 2400 (0.92 PFLOP/s; no cap 2000, a cap of 20, whose logits leave the short polynomial, 2750); 16 prompts of 33 .. 2048 under a
-// window 94; 6 of 101 .. 3001, 8 heads of 64, a bias and prefixes 39.
+// of 50 2400 to 2470 (0.92 to 0.89 PFLOP/s; no cap 2060, a cap of 20, whose logits leave the short polynomial, 2850); 16 prompts of 33 ..
+// 2048 under a window 89; 6 of 101 .. 3001, 8 heads of 64, a bias and prefixes 39.
 #include "prompt.h"
 #include "score_rule.h"
 
@@ -440,11 +446,12 @@ pbs_status launch_rows(const RuleArgs &a, long long grid, hipStream_t s)
 template <int D>
 pbs_status launch_rule(RuleArgs &a, long long grid, hipStream_t s)
 {
-    // 256 rows to a workgroup where that leaves two of them and more to a compute unit.  Measured, us, 256 rows / 128 in halves, 32 / 8 heads of
-    // 128 under a cap: 2000 tokens (256 workgroups) 79 / 58, 4000 (504) 199 / 213, 8000 (1000) 625 / 663; a window of 512, 8 prompts of
-    // 33 .. 2048 (552) 57 / 71, 16 of them 96 / 121.  A head to every kv head makes rows tokens, and 256 of them see more that is hidden: 8
-    // heads of 64 with a bias, prompts of 2000 .. 6000, 4 (528) 157 / 143, 8 (1050) 269 / 232, 16 (2080) 430 / 427, those of heads of 128
-    // 607 / 639.
+    // 256 rows to a workgroup where kWide of them or more are left, 1.75 to a compute unit.  Measured, us, 256 rows / 128 in halves, 32 / 8 heads
+    // of 128 under a cap: 2000 tokens (256 workgroups) 74 / 60, 2800 (352) 98 / 96, 3200 (408) 113 / 116, 3600 (456) 130 / 144, 4000 (504)
+    // 156 / 171, 8000 (1008) 574 / 613; 6 prompts of 500 (416) 39 / 39, 44 of 60 (680) 20 / 28; a window of 512, prompts of 33 .. 2048, 2
+    // (272) 28 / 35, 8 (1104) 93 / 117.  A head to every kv head makes rows tokens, and 256 of them see more that is hidden: four times as
+    // many are asked for.  8 heads with a bias, prompts of 2000 .. 6000, heads of 64, 4 (528) 168 / 134, 8 (1056) 283 / 244, 14 (1856)
+    // 451 / 419, 24 (3184) 732 / 713, heads of 128, 8 (1056) 388 / 358, 14 (1856) 629 / 633; 150 of 60, heads of 64 (1480) 30 / 35.
     const int tokens = 2 * kRows / a.r;
     const long long wide = ((long long)a.total_q / tokens + a.n_seq) * a.h_kv;
     if (wide < (a.r == 1 ? 4 * kWide : kWide)) return launch_rows<D, true>(a, grid, s);
