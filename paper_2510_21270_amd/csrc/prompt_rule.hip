@@ -23,7 +23,7 @@
 // 6 with a bias and prefixes 39 -> 47, 4 of 1 .. 200 11.1 -> 11.9.
 //
 // Issue slots bound the long prompts, starts and ends of workgroups the short ones.  Measured, us, 32 / 8 heads of 128: 16384 tokens under a cap
-// of 50 2400 to 2470 (0.92 to 0.89 PFLOP/s; no cap 2060, a cap of 20, whose logits leave the short polynomial, 2850); 16 prompts of 33 ..
+// of 50 2400 to 2580, by the card's clock (0.92 to 0.85 PFLOP/s; no cap 2060, a cap of 20, whose logits leave the short polynomial, 2850); 16 prompts of 33 ..
 // 2048 under a window 89; 6 of 101 .. 3001, 8 heads of 64, a bias and prefixes 39.
 #include "prompt.h"
 #include "score_rule.h"
